@@ -232,7 +232,7 @@ def prepare(case, seed):
             from paper_2509_26246_amd import harness as H
             s["rotary"] = H.Rotary(case["hq"], case["hkv"], case["d"], _dtype(case), s["inv_freq"], q_weight=s["wq"], k_weight=s["wk"],
                                    norm=case["norm"], eps=EPS, rotary_dim=case["rotary"], sections=_sections(case), dealt=case["dealt"],
-                                   adjacent=case["adjacent"], max_tokens=case["tokens"])
+                                   adjacent=case["adjacent"])
             s["out"] = [torch.empty_like(s[x], memory_format=torch.contiguous_format) for x in "qk"]
             if case["backward"]:
                 heads = case["hq"] + (2 if case["fused"] else 1) * case["hkv"]
