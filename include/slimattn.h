@@ -398,6 +398,53 @@ int slimattn_bwd_static(const slimattn_params* p, const void* q, const void* k, 
                         const float* lse, const void* dO, const slimattn_tables* t, void* dQ, void* dK,
                         void* dV, void* stream);
 
+/* ---- queries and keys before attention: norm per head and rotation ----------------------------------- */
+
+#define SLIMATTN_ROPE_NORM      1   /* norm of each head before the rotation */
+#define SLIMATTN_ROPE_ADJACENT  2   /* pairs are (2i, 2i + 1); otherwise (i, i + rotary_dim / 2) */
+#define SLIMATTN_ROPE_DEALT     4   /* pairs are dealt to the axes in turn; otherwise each axis has a block of neighbouring pairs */
+
+typedef struct slimattn_rope_params {
+  int32_t total_tokens;           /* T */
+  int32_t n_q_heads, n_kv_heads;  /* Hq, Hkv >= 0, not both 0 (0: no queries or no keys; their pointers are not looked at) */
+  int32_t head_dim;               /* d: 16, 32, 64 or 128 */
+  int32_t dtype;                  /* SLIMATTN_F32 or SLIMATTN_BF16: the tensors; weights are float, arithmetic is fp32 */
+  int32_t rotary_dim;             /* channels 0 .. rotary_dim - 1 of a head are rotated, the others pass: a multiple of 8 up to d;
+                                     0 (the norm alone) with SLIMATTN_ROPE_NORM */
+  int32_t n_axes;                 /* 1 .. 4 axes of positions (time, height, width, ...); not looked at if rotary_dim is 0 */
+  int32_t sections[4];            /* pairs of each axis, rotary_dim / 2 together */
+  float   eps;                    /* added to the mean square, 2^-100 .. 2^100 with SLIMATTN_ROPE_NORM */
+  int32_t flags;                  /* SLIMATTN_ROPE_* */
+  int64_t q_stride, k_stride;     /* elements from one token of q (k) to the next, 0: packed, else >= heads * d and a multiple of
+                                     16 bytes: the columns of a fused projection are read where they are */
+  int64_t dq_stride, dk_stride;   /* the same for dq and dk (slimattn_rope_bwd) */
+} slimattn_rope_params;
+
+/* Norm of every query and key head, then rotation by the token's positions, in one pass over the tensors:
+ *   n_c = x_c * w_c / sqrt(mean_c x_c^2 + eps)                         (SLIMATTN_ROPE_NORM; otherwise n = x)
+ *   (a, b) of pair i  ->  (a cos t - b sin t, b cos t + a sin t),  t = positions[axis of pair i][token] * inv_freq[i].
+ * With SLIMATTN_ROPE_DEALT the axes take one pair each in turn, axis 0 first, as long as they have pairs left.  Angles are formed in
+ * 64 bits and turned into (-pi/4, pi/4] before they are rounded: any int32 position is as exact as a small one.
+ * q [T, Hq, d] by q_stride, k [T, Hkv, d] by k_stride -> q_out, k_out packed, as slimattn_fwd reads them.  q_weight, k_weight float [d]
+ * (SLIMATTN_ROPE_NORM; NULL: ones); positions int32 [n_axes, T]; inv_freq float [rotary_dim / 2].  All DEVICE; tensors 16-byte
+ * aligned, the rest 4-byte.  q_out may be q (k_out be k) where that is packed; other overlaps of an output are refused.
+ * Allocates nothing, does not synchronise, one kernel launch. */
+int slimattn_rope_fwd(const slimattn_rope_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                      const int32_t* positions, const float* inv_freq, void* q_out, void* k_out, void* stream);
+
+/* Bytes of DEVICE scratch slimattn_rope_bwd needs (partial sums of the weights' gradients; the same for any total_tokens;
+ * 0 without SLIMATTN_ROPE_NORM or for parameters that it refuses).  Its contents need no initialisation; calls that overlap in time need one each. */
+size_t slimattn_rope_bwd_workspace_bytes(const slimattn_rope_params* p);
+
+/* Gradients of slimattn_rope_fwd: dq_out [T, Hq, d], dk_out [T, Hkv, d] packed (as slimattn_bwd writes dQ, dK) -> dq, dk by dq_stride,
+ * dk_stride, and with SLIMATTN_ROPE_NORM dq_weight, dk_weight float [d], summed over tokens and heads in a fixed order (no atomics; bitwise
+ * repeatable) and overwritten; either may be NULL.  q, k are the inputs of the forward pass (read with SLIMATTN_ROPE_NORM only).
+ * dq may be dq_out or q (dk be dk_out or k) where their strides are the same; other overlaps of an output are refused.
+ * Allocates nothing, does not synchronise; one kernel launch, two with weight gradients. */
+int slimattn_rope_bwd(const slimattn_rope_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                      const int32_t* positions, const float* inv_freq, const void* dq_out, const void* dk_out, void* dq, void* dk,
+                      float* dq_weight, float* dk_weight, void* workspace, void* stream);
+
 /* ---- measurement aid --------------------------------------------------------------------------- */
 
 /* Kernel classes reported by slimattn_profile_read. */

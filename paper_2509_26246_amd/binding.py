@@ -13,6 +13,7 @@ LIB_PATH = os.path.join(HERE, "libslimattn.so")
 F32, BF16 = 0, 1
 FLAG_PER_UNIT_LAUNCH = 1
 FLAG_STATS_PREPASS = 2
+ROPE_NORM, ROPE_ADJACENT, ROPE_DEALT = 1, 2, 4
 CHECK_FORWARD, CHECK_BACKWARD, CHECK_ORDER = 0, 1, 2
 POLICY_KINDS = {"ALL": 0, "PER_SAMPLE": 1, "ROUND_ROBIN": 2, "PREFIX_FILL": 3, "TOKEN_CAP": 4, "SEEDED_LPT": 5,
                 "ISOLATE_FILL": 6}
@@ -21,7 +22,8 @@ EXPORTED_SYMBOLS = [
     "slimattn_solve_partition", "slimattn_solve_bottlenecks", "slimattn_dag_timeline", "slimattn_dag_build_1f1b", "slimattn_dag_memory", "slimattn_dag_buffers_1f1b", "slimattn_candidate_unit_counts", "slimattn_search_unit_count", "slimattn_shape_supported", "slimattn_slice_pairs", "slimattn_flops_fwd", "slimattn_flops_bwd", "slimattn_tables_create", "slimattn_tables_create_async",
     "slimattn_tables_destroy", "slimattn_tables_count", "slimattn_bwd_workspace_bytes", "slimattn_fwd", "slimattn_fwd_divided_counts",
     "slimattn_bwd", "slimattn_bwd_static", "slimattn_bwd_released_rows", "slimattn_bwd_dkdv_plan", "slimattn_strerror", "slimattn_last_hip_error", "slimattn_version", "slimattn_profile_enable",
-    "slimattn_profile_read", "slimattn_profile_read_launches"]
+    "slimattn_profile_read", "slimattn_profile_read_launches",
+    "slimattn_rope_fwd", "slimattn_rope_bwd", "slimattn_rope_bwd_workspace_bytes"]
 KERNEL_CLASSES = ["fwd", "delta", "dq", "dkdv", "reduce", "unused", "fwd_call", "bwd_call"]
 
 
@@ -47,6 +49,12 @@ class _Params(C.Structure):
     _fields_ = [("total_tokens", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("unit_lo", C.c_int32),
                 ("unit_hi", C.c_int32), ("flags", C.c_int32)]
+
+
+class _RopeParams(C.Structure):
+    _fields_ = [("total_tokens", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("rotary_dim", C.c_int32), ("n_axes", C.c_int32), ("sections", C.c_int32 * 4), ("eps", C.c_float),
+                ("flags", C.c_int32), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("dq_stride", C.c_int64), ("dk_stride", C.c_int64)]
 
 
 _lib = None
@@ -100,6 +108,10 @@ def load_library():
     lib.slimattn_bwd_released_rows.argtypes = [vp, C.c_int32, i32p, C.c_int32, i32p]
     lib.slimattn_bwd_dkdv_plan.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, i32p]
     lib.slimattn_fwd_divided_counts.argtypes = [C.POINTER(C.c_int64)]
+    lib.slimattn_rope_fwd.argtypes = [C.POINTER(_RopeParams)] + [vp] * 9
+    lib.slimattn_rope_bwd.argtypes = [C.POINTER(_RopeParams)] + [vp] * 14
+    lib.slimattn_rope_bwd_workspace_bytes.argtypes = [C.POINTER(_RopeParams)]
+    lib.slimattn_rope_bwd_workspace_bytes.restype = C.c_size_t
     lib.slimattn_strerror.argtypes = [C.c_int]
     lib.slimattn_strerror.restype = C.c_char_p
     lib.slimattn_last_hip_error.restype = C.c_int
@@ -468,6 +480,107 @@ def bwd_dkdv_plan(tables: Tables, n_q_heads: int, n_kv_heads: int, head_dim: int
     if rc != 0:
         raise SlimAttnError(rc, "slimattn_bwd_dkdv_plan")
     return tuple(int(x) for x in plan)
+
+
+def _check_tensor(t, dtype: str, numel: int, what: str) -> None:
+    """A torch tensor that a kernel will take as `numel` elements of `dtype`, on the current device."""
+    if str(t.dtype) != "torch." + dtype:
+        raise ValueError(f"{what}: {t.dtype}, expected torch.{dtype}")
+    if t.numel() < numel:
+        raise ValueError(f"{what}: {t.numel()} elements, expected {numel}")
+    if not t.is_cuda or t.device.index != _current_device():
+        raise ValueError(f"{what}: on {t.device}, expected the current GPU")
+
+
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+_TORCH_DTYPE = {F32: "float32", BF16: "bfloat16"}
+
+
+def _opt_ptr(t, dtype: str, numel: int, what: str):
+    """_ptr of a contiguous tensor of at least `numel` elements, a raw address, or None."""
+    if t is None or isinstance(t, int):
+        return t
+    _check_tensor(t, dtype, numel, what)
+    return _ptr(t)
+
+
+def _rows_ptr(t, T: int, heads: int, d: int, dtype: int, stride: int, what: str):
+    """(address, elements from token to token) of a [T, heads, d] tensor whose heads lie one behind the other (a raw address: `stride`)."""
+    if t is None or isinstance(t, int):
+        return t, stride
+    if tuple(t.shape) != (T, heads, d):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(T, heads, d)}")
+    _check_tensor(t, _TORCH_DTYPE.get(dtype, str(dtype)), 0, what)
+    if T == 0 or heads == 0:
+        return t.data_ptr(), 0
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{what}: the heads of a token must lie one behind the other")
+    return t.data_ptr(), t.stride(0) if T > 1 else 0
+
+
+def _rope_params(T, hq, hkv, d, dtype, rotary_dim, sections, eps, flags) -> _RopeParams:
+    p = _RopeParams(total_tokens=T, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, dtype=dtype, rotary_dim=rotary_dim, n_axes=len(sections),
+                    eps=eps, flags=flags)
+    if len(sections) <= 4:                                      # (the library refuses more axes)
+        p.sections = (C.c_int32 * 4)(*sections)
+    return p
+
+
+def _rope_small(q_weight, k_weight, positions, inv_freq, T, d, rotary_dim, n_axes):
+    return (_opt_ptr(q_weight, "float32", d, "q_weight"), _opt_ptr(k_weight, "float32", d, "k_weight"),
+            _opt_ptr(positions, "int32", n_axes * T, "positions"), _opt_ptr(inv_freq, "float32", rotary_dim // 2, "inv_freq"))
+
+
+def rope_fwd(q, k, positions, inv_freq, q_out, k_out, *, total_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int,
+             rotary_dim: int, sections: Sequence[int], q_weight=None, k_weight=None, eps: float = 1e-6, flags: int = 0, q_stride: int = 0,
+             k_stride: int = 0, stream: Optional[int] = None) -> None:
+    """slimattn_rope_fwd: q, k [T, heads, d] (rows any distance apart, for raw addresses q_stride, k_stride) -> q_out, k_out packed."""
+    lib = load_library()
+    p = _rope_params(total_tokens, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, sections, eps, flags)
+    dims = (total_tokens, head_dim, dtype)
+    pq, p.q_stride = _rows_ptr(q, dims[0], n_q_heads, *dims[1:], q_stride, "q")
+    pk, p.k_stride = _rows_ptr(k, dims[0], n_kv_heads, *dims[1:], k_stride, "k")
+    n = total_tokens * head_dim
+    rc = lib.slimattn_rope_fwd(C.byref(p), pq, pk, *_rope_small(q_weight, k_weight, positions, inv_freq, total_tokens, head_dim, rotary_dim, len(sections)),
+                               _opt_ptr(q_out, _TORCH_DTYPE.get(dtype), n * n_q_heads, "q_out"),
+                               _opt_ptr(k_out, _TORCH_DTYPE.get(dtype), n * n_kv_heads, "k_out"), stream)
+    _raise(rc, "slimattn_rope_fwd")
+
+
+def rope_bwd_workspace_bytes(total_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, rotary_dim: int,
+                             sections: Sequence[int], eps: float = 1e-6, flags: int = 0) -> int:
+    p = _rope_params(total_tokens, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, sections, eps, flags)
+    return int(load_library().slimattn_rope_bwd_workspace_bytes(C.byref(p)))
+
+
+def rope_bwd(q, k, positions, inv_freq, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, *, total_tokens: int, n_q_heads: int,
+             n_kv_heads: int, head_dim: int, dtype: int, rotary_dim: int, sections: Sequence[int], q_weight=None, k_weight=None,
+             eps: float = 1e-6, flags: int = 0, q_stride: int = 0, k_stride: int = 0, dq_stride: int = 0, dk_stride: int = 0,
+             stream: Optional[int] = None) -> None:
+    """slimattn_rope_bwd: dq_out, dk_out packed -> dq, dk (rows any distance apart) and, with ROPE_NORM, dq_weight, dk_weight."""
+    lib = load_library()
+    p = _rope_params(total_tokens, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, sections, eps, flags)
+    T, d = total_tokens, head_dim
+    pq, p.q_stride = _rows_ptr(q, T, n_q_heads, d, dtype, q_stride, "q")
+    pk, p.k_stride = _rows_ptr(k, T, n_kv_heads, d, dtype, k_stride, "k")
+    pdq, p.dq_stride = _rows_ptr(dq, T, n_q_heads, d, dtype, dq_stride, "dq")
+    pdk, p.dk_stride = _rows_ptr(dk, T, n_kv_heads, d, dtype, dk_stride, "dk")
+    need = int(lib.slimattn_rope_bwd_workspace_bytes(C.byref(p))) if dq_weight is not None or dk_weight is not None else 0
+    rc = lib.slimattn_rope_bwd(C.byref(p), pq, pk, *_rope_small(q_weight, k_weight, positions, inv_freq, T, d, rotary_dim, len(sections)),
+                               _opt_ptr(dq_out, _TORCH_DTYPE.get(dtype), T * d * n_q_heads, "dq_out"),
+                               _opt_ptr(dk_out, _TORCH_DTYPE.get(dtype), T * d * n_kv_heads, "dk_out"), pdq, pdk,
+                               _opt_ptr(dq_weight, "float32", d, "dq_weight"), _opt_ptr(dk_weight, "float32", d, "dk_weight"),
+                               _opt_ptr(workspace, "uint8", need, "workspace"), stream)
+    _raise(rc, "slimattn_rope_bwd")
+
+
+def _raise(rc: int, where: str) -> None:
+    if rc != 0:
+        raise SlimAttnError(rc, where, f" hip={load_library().slimattn_last_hip_error()}" if rc == -4 else "")
 
 
 STATIC_SCRATCH_BYTES = 64 << 20

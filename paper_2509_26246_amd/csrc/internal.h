@@ -318,4 +318,11 @@ int prepare_static_scratch();
 int fwd_q_tile(int dtype, int head_dim);
 int dq_q_tile(int dtype, int head_dim);
 int dkdv_kv_tile(int dtype, int head_dim);
+// ---- norm and rotation of queries and keys (rope.hip); arguments checked by the entry points ----
+size_t rope_partial_bytes(const slimattn_rope_params& p);
+int launch_rope_fwd(const slimattn_rope_params& p, const void* q, const void* k, const float* qw, const float* kw, const int32_t* pos,
+                    const float* freq, void* qo, void* ko, void* stream);
+int launch_rope_bwd(const slimattn_rope_params& p, const void* q, const void* k, const float* qw, const float* kw, const int32_t* pos,
+                    const float* freq, const void* gq, const void* gk, void* dq, void* dk, float* dqw, float* dkw, void* ws, void* stream);
+
 }  // namespace slimattn

@@ -3,7 +3,7 @@ every computation is a call into libslimattn."""
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import Optional
+from typing import Optional, Sequence
 
 import numpy as np
 import torch
@@ -101,3 +101,46 @@ def make_problem(q: np.ndarray, k: np.ndarray, v: np.ndarray, dO: np.ndarray, cu
                    torch.empty((T, hq, d), dtype=tdt, device=device), torch.empty((hq, T), dtype=torch.float32, device=device),
                    torch.empty((T, hq, d), dtype=tdt, device=device), torch.empty((T, hkv, d), dtype=tdt, device=device),
                    torch.empty((T, hkv, d), dtype=tdt, device=device), ws)
+
+
+def _lib_dtype(dtype: torch.dtype) -> int:
+    if dtype == torch.bfloat16:
+        return B.BF16
+    if dtype == torch.float32:
+        return B.F32
+    raise ValueError(f"{dtype}: expected torch.bfloat16 or torch.float32")
+
+
+class Rotary:
+    """Norm per head and rotation of a layer's queries and keys, in front of slimattn_fwd, and their gradients behind slimattn_bwd: the
+    parameters of the layer and what its backward pass needs (workspace, weight gradients), for calls of any number of tokens."""
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, inv_freq: Optional[torch.Tensor], *,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, norm: bool = False, eps: float = 1e-6,
+                 rotary_dim: Optional[int] = None, sections: Optional[Sequence[int]] = None, dealt: bool = False, adjacent: bool = False,
+                 device="cuda"):
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
+        self.inv_freq, self.q_weight, self.k_weight, self.norm = inv_freq, q_weight, k_weight, norm
+        rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        self._shape = dict(n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=_lib_dtype(dtype), rotary_dim=rotary_dim,
+                           sections=list(sections) if sections is not None else [rotary_dim // 2], eps=eps,
+                           flags=B.ROPE_NORM * norm | B.ROPE_ADJACENT * adjacent | B.ROPE_DEALT * dealt)
+        self.dq_weight = self.dk_weight = self.workspace = None
+        if norm:
+            need = B.rope_bwd_workspace_bytes(0, **self._shape)
+            self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+            self.dq_weight = torch.zeros(head_dim, dtype=torch.float32, device=device)
+            self.dk_weight = torch.zeros(head_dim, dtype=torch.float32, device=device)
+
+    def _kw(self, tokens: int):
+        return dict(self._shape, total_tokens=tokens, q_weight=self.q_weight, k_weight=self.k_weight,
+                    stream=torch.cuda.current_stream().cuda_stream)
+
+    def forward(self, q, k, positions, q_out, k_out):
+        """q, k [T, heads, d] (columns of a fused projection, or packed), positions int32 [axes, T] or [T] -> q_out, k_out, packed."""
+        B.rope_fwd(q, k, positions, self.inv_freq, q_out, k_out, **self._kw((q if q is not None else k).shape[0]))
+
+    def backward(self, q, k, positions, dq_out, dk_out, dq, dk):
+        """dQ, dK of the attention and the forward's inputs -> dq, dk; the weights' gradients go to dq_weight, dk_weight."""
+        B.rope_bwd(q, k, positions, self.inv_freq, dq_out, dk_out, dq, dk, self.dq_weight, self.dk_weight, self.workspace,
+                   **self._kw((dq_out if dq_out is not None else dk_out).shape[0]))
