@@ -445,6 +445,59 @@ int slimattn_rope_bwd(const slimattn_rope_params* p, const void* q, const void* 
                       const int32_t* positions, const float* inv_freq, const void* dq_out, const void* dk_out, void* dq, void* dk,
                       float* dq_weight, float* dk_weight, void* workspace, void* stream);
 
+/* ---- a key/value cache in 4 bits ------------------------------------------------------------------------ */
+
+/* Keys and values of sequences that grow, in pages of page_size tokens; a page holds all KV heads.  32 neighbouring channels of a token's
+ * head share a scale: s = max |x| / 6 rounded to six significant bits (ties to even; 0 below max |x| = 2^-100, at most 1.3125 * 2^125);
+ * a value is s times the 4-bit float (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) nearest to x / s, ties to the even code.  4.5 bits
+ * a value; every value is exactly a bf16 number.  32 channels with an infinity or a NaN among them read back as NaN.
+ * The bytes of a page are the library's own affair: they are written by slimattn_cache_write and moved by whole pages only. */
+typedef struct slimattn_cache_params {
+  int32_t n_pages;                /* pages in the cache, >= 1 */
+  int32_t page_size;              /* tokens: 16, 32, 64, 128 or 256 */
+  int32_t n_kv_heads, head_dim;   /* Hkv; d: 64 or 128 */
+  int32_t dtype;                  /* SLIMATTN_F32 or SLIMATTN_BF16: k, v, q, o */
+  int32_t n_seqs;                 /* sequences, 0 .. 65536 */
+  int32_t max_pages;              /* columns of the page table, >= 1; max_pages * page_size < 2^31 */
+  int32_t n_rows;                 /* rows of k, v, q, o */
+} slimattn_cache_params;
+
+/* The calls below share these DEVICE int32 arrays, which they read when they run (a recorded call follows what the arrays then hold):
+ *   lens [n_seqs]                   tokens of each sequence, the rows of this call included;
+ *   row_ptr [n_seqs + 1] or NULL    rows row_ptr[b] .. row_ptr[b+1] - 1 of the tensors are the last tokens of sequence b, in order: of its
+ *                                   n rows the i-th stands at position lens[b] - n + i.  Ascending.  NULL: one row each (n_rows = n_seqs);
+ *   page_table [n_seqs, max_pages]  page_table[b][j] holds positions j * page_size ... of sequence b.  Entries past its length are not read.
+ * Their contents cannot be checked before a launch.  Whatever they hold, nothing outside the tensors and the cache is touched: lengths
+ * are taken as 0 .. max_pages * page_size; a row at a negative position is not written, reads as zeros, and sees nothing (o = 0,
+ * lse = -inf); a page index outside 0 .. n_pages - 1 is a page that is not there: not written, read as zeros, its keys not seen.  Rows before
+ * row_ptr[0] and from row_ptr[n_seqs] on are left as they were.  Two rows of one call must not write the same position of a page.
+ * All: 16-byte aligned tensors, cache and workspace; nothing allocated, no synchronisation, kernel launches only. */
+
+/* Bytes of the cache (DEVICE; needs no initialisation).  0 for a shape that the calls refuse. */
+size_t slimattn_cache_bytes(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
+
+/* k, v [n_rows, Hkv, d], k_stride and v_stride elements from row to row (0: packed; else >= Hkv * d and a multiple of 16 bytes), into
+ * the cache: beside slimattn_rope_fwd in front of slimattn_cache_attn, or after a prefill by slimattn_fwd. */
+int slimattn_cache_write(const slimattn_cache_params* p, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                         const int32_t* row_ptr, const int32_t* lens, const int32_t* page_table, void* cache, void* stream);
+
+/* The cache's values of the rows, k, v [n_rows, Hkv, d] packed, as slimattn_fwd reads them (a later slice of a long prompt whose earlier
+ * ones are in the cache).  Rounds nothing. */
+int slimattn_cache_read(const slimattn_cache_params* p, const void* cache, const int32_t* row_ptr, const int32_t* lens,
+                        const int32_t* page_table, void* k, void* v, void* stream);
+
+/* Bytes of DEVICE scratch slimattn_cache_attn needs.  Its contents need no initialisation; calls that overlap in time need one each.
+ * 0 for parameters that slimattn_cache_attn refuses. */
+size_t slimattn_cache_attn_workspace_bytes(const slimattn_cache_params* p, int32_t n_q_heads);
+
+/* Attention of the rows over their sequences' caches: the row at position p sees keys 0 .. p,
+ * S_j = scale * q . k_j, lse = log sum_j exp S_j, o = sum_j exp(S_j - lse) v_j.  q, o [n_rows, Hq, d] packed, Hq a multiple of Hkv (query head h
+ * uses KV head h / (Hq / Hkv)); lse float [Hq, n_rows] or NULL; o must not overlap q.  The keys of long sequences are divided among blocks
+ * and the parts added in their order: the same call on the same inputs gives the same bits.  Two launches, one where a single block does. */
+int slimattn_cache_attn(const slimattn_cache_params* p, int32_t n_q_heads, float scale, const void* q, const int32_t* row_ptr,
+                        const int32_t* lens, const int32_t* page_table, const void* cache, void* o, float* lse, void* workspace,
+                        void* stream);
+
 /* ---- measurement aid --------------------------------------------------------------------------- */
 
 /* Kernel classes reported by slimattn_profile_read. */

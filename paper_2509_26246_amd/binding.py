@@ -23,7 +23,8 @@ EXPORTED_SYMBOLS = [
     "slimattn_tables_destroy", "slimattn_tables_count", "slimattn_bwd_workspace_bytes", "slimattn_fwd", "slimattn_fwd_divided_counts",
     "slimattn_bwd", "slimattn_bwd_static", "slimattn_bwd_released_rows", "slimattn_bwd_dkdv_plan", "slimattn_strerror", "slimattn_last_hip_error", "slimattn_version", "slimattn_profile_enable",
     "slimattn_profile_read", "slimattn_profile_read_launches",
-    "slimattn_rope_fwd", "slimattn_rope_bwd", "slimattn_rope_bwd_workspace_bytes"]
+    "slimattn_rope_fwd", "slimattn_rope_bwd", "slimattn_rope_bwd_workspace_bytes",
+    "slimattn_cache_bytes", "slimattn_cache_write", "slimattn_cache_read", "slimattn_cache_attn", "slimattn_cache_attn_workspace_bytes"]
 KERNEL_CLASSES = ["fwd", "delta", "dq", "dkdv", "reduce", "unused", "fwd_call", "bwd_call"]
 
 
@@ -55,6 +56,11 @@ class _RopeParams(C.Structure):
     _fields_ = [("total_tokens", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("dtype", C.c_int32), ("rotary_dim", C.c_int32), ("n_axes", C.c_int32), ("sections", C.c_int32 * 4), ("eps", C.c_float),
                 ("flags", C.c_int32), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("dq_stride", C.c_int64), ("dk_stride", C.c_int64)]
+
+
+class _CacheParams(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("n_rows", C.c_int32)]
 
 
 _lib = None
@@ -112,6 +118,13 @@ def load_library():
     lib.slimattn_rope_bwd.argtypes = [C.POINTER(_RopeParams)] + [vp] * 14
     lib.slimattn_rope_bwd_workspace_bytes.argtypes = [C.POINTER(_RopeParams)]
     lib.slimattn_rope_bwd_workspace_bytes.restype = C.c_size_t
+    lib.slimattn_cache_bytes.argtypes = [C.c_int32] * 4
+    lib.slimattn_cache_bytes.restype = C.c_size_t
+    lib.slimattn_cache_write.argtypes = [C.POINTER(_CacheParams), vp, vp, C.c_int64, C.c_int64] + [vp] * 5
+    lib.slimattn_cache_read.argtypes = [C.POINTER(_CacheParams)] + [vp] * 7
+    lib.slimattn_cache_attn.argtypes = [C.POINTER(_CacheParams), C.c_int32, C.c_float] + [vp] * 9
+    lib.slimattn_cache_attn_workspace_bytes.argtypes = [C.POINTER(_CacheParams), C.c_int32]
+    lib.slimattn_cache_attn_workspace_bytes.restype = C.c_size_t
     lib.slimattn_strerror.argtypes = [C.c_int]
     lib.slimattn_strerror.restype = C.c_char_p
     lib.slimattn_last_hip_error.restype = C.c_int
@@ -576,6 +589,61 @@ def rope_bwd(q, k, positions, inv_freq, dq_out, dk_out, dq, dk, dq_weight, dk_we
                                _opt_ptr(dq_weight, "float32", d, "dq_weight"), _opt_ptr(dk_weight, "float32", d, "dk_weight"),
                                _opt_ptr(workspace, "uint8", need, "workspace"), stream)
     _raise(rc, "slimattn_rope_bwd")
+
+
+def _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows) -> _CacheParams:
+    return _CacheParams(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+
+
+def cache_bytes(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int) -> int:
+    """slimattn_cache_bytes: size of the cache, 0 for a shape that is refused."""
+    return int(load_library().slimattn_cache_bytes(n_pages, page_size, n_kv_heads, head_dim))
+
+
+def _cache_arrays(p: _CacheParams, cache, page_table, lens, row_ptr):
+    """Addresses (row_ptr, lens, page_table, cache), the tensors among them checked."""
+    return (_opt_ptr(row_ptr, "int32", p.n_seqs + 1, "row_ptr"), _opt_ptr(lens, "int32", p.n_seqs, "lens"),
+            _opt_ptr(page_table, "int32", p.n_seqs * p.max_pages, "page_table"),
+            _opt_ptr(cache, "uint8", 0 if isinstance(cache, int) else cache_bytes(p.n_pages, p.page_size, p.n_kv_heads, p.head_dim), "cache"))
+
+
+def cache_write(k, v, cache, page_table, lens, row_ptr=None, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
+                dtype: int, n_seqs: int, max_pages: int, k_stride: int = 0, v_stride: int = 0, stream: Optional[int] = None) -> None:
+    """slimattn_cache_write: k, v [n_rows, Hkv, d] (rows any distance apart, for raw addresses k_stride, v_stride) into the cache."""
+    p = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+    pk, k_stride = _rows_ptr(k, n_rows, n_kv_heads, head_dim, dtype, k_stride, "k")
+    pv, v_stride = _rows_ptr(v, n_rows, n_kv_heads, head_dim, dtype, v_stride, "v")
+    rp, ln, pt, ca = _cache_arrays(p, cache, page_table, lens, row_ptr)
+    _raise(load_library().slimattn_cache_write(C.byref(p), pk, pv, k_stride, v_stride, rp, ln, pt, ca, stream), "slimattn_cache_write")
+
+
+def cache_read(cache, page_table, lens, k, v, row_ptr=None, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
+               dtype: int, n_seqs: int, max_pages: int, stream: Optional[int] = None) -> None:
+    """slimattn_cache_read: the cache's values of the rows -> k, v [n_rows, Hkv, d] packed."""
+    p = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+    rp, ln, pt, ca = _cache_arrays(p, cache, page_table, lens, row_ptr)
+    n, name = n_rows * n_kv_heads * head_dim, _TORCH_DTYPE.get(dtype)
+    _raise(load_library().slimattn_cache_read(C.byref(p), ca, rp, ln, pt, _opt_ptr(k, name, n, "k"), _opt_ptr(v, name, n, "v"), stream),
+           "slimattn_cache_read")
+
+
+def cache_attn_workspace_bytes(n_q_heads: int, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: int,
+                               n_seqs: int, max_pages: int) -> int:
+    p = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+    return int(load_library().slimattn_cache_attn_workspace_bytes(C.byref(p), n_q_heads))
+
+
+def cache_attn(q, cache, page_table, lens, o, lse, workspace, row_ptr=None, *, n_q_heads: int, scale: float, n_rows: int, n_pages: int,
+               page_size: int, n_kv_heads: int, head_dim: int, dtype: int, n_seqs: int, max_pages: int, stream: Optional[int] = None) -> None:
+    """slimattn_cache_attn: q [n_rows, Hq, d] over the cache -> o, and lse [Hq, n_rows] unless it is None."""
+    lib = load_library()
+    p = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+    rp, ln, pt, ca = _cache_arrays(p, cache, page_table, lens, row_ptr)
+    n, name = n_rows * n_q_heads * head_dim, _TORCH_DTYPE.get(dtype)
+    need = int(lib.slimattn_cache_attn_workspace_bytes(C.byref(p), n_q_heads))
+    rc = lib.slimattn_cache_attn(C.byref(p), n_q_heads, scale, _opt_ptr(q, name, n, "q"), rp, ln, pt, ca, _opt_ptr(o, name, n, "o"),
+                                 _opt_ptr(lse, "float32", n_rows * n_q_heads, "lse"), _opt_ptr(workspace, "uint8", need, "workspace"), stream)
+    _raise(rc, "slimattn_cache_attn")
 
 
 def _raise(rc: int, where: str) -> None:

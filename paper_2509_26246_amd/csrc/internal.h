@@ -325,4 +325,13 @@ int launch_rope_fwd(const slimattn_rope_params& p, const void* q, const void* k,
 int launch_rope_bwd(const slimattn_rope_params& p, const void* q, const void* k, const float* qw, const float* kw, const int32_t* pos,
                     const float* freq, const void* gq, const void* gk, void* dq, void* dk, float* dqw, float* dkw, void* ws, void* stream);
 
+// ---- the 4-bit cache (cache.hip, cache_attn.hip); arguments checked by the entry points ----
+int launch_cache_write(const slimattn_cache_params& p, const void* k, const void* v, int64_t k_stride, int64_t v_stride, const int32_t* row_ptr,
+                       const int32_t* lens, const int32_t* table, void* cache, void* stream);
+int launch_cache_read(const slimattn_cache_params& p, const void* cache, const int32_t* row_ptr, const int32_t* lens, const int32_t* table, void* k,
+                      void* v, void* stream);
+size_t cache_attn_bytes(const slimattn_cache_params& p, int n_q_heads);
+int launch_cache_attn(const slimattn_cache_params& p, int n_q_heads, float scale, const void* q, const int32_t* row_ptr, const int32_t* lens,
+                      const int32_t* table, const void* cache, void* o, float* lse, void* ws, void* stream);
+
 }  // namespace slimattn

@@ -144,3 +144,38 @@ class Rotary:
         """dQ, dK of the attention and the forward's inputs -> dq, dk; the weights' gradients go to dq_weight, dk_weight."""
         B.rope_bwd(q, k, positions, self.inv_freq, dq_out, dk_out, dq, dk, self.dq_weight, self.dk_weight, self.workspace,
                    **self._kw((dq_out if dq_out is not None else dk_out).shape[0]))
+
+
+class KVCache:
+    """One layer's keys and values of a batch of sequences in 4 bits: the pages, the page table and the lengths (device tensors the program
+    updates as sequences grow), and the workspace of attention calls of up to `max_rows` rows."""
+
+    def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, page_table: torch.Tensor,
+                 lens: torch.Tensor, *, max_rows: int = 0, n_q_heads: int = 0):
+        self.page_table, self.lens, self.n_q_heads = page_table, lens, n_q_heads
+        self._shape = dict(n_pages=n_pages, page_size=page_size, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=_lib_dtype(dtype),
+                           n_seqs=page_table.shape[0], max_pages=page_table.shape[1])
+        size = B.cache_bytes(n_pages, page_size, n_kv_heads, head_dim)
+        if size == 0:
+            raise ValueError("cache: unsupported pages or heads")
+        self.cache = torch.empty(size, dtype=torch.uint8, device=page_table.device)
+        self.workspace = None
+        if n_q_heads:
+            need = B.cache_attn_workspace_bytes(n_q_heads, n_rows=max_rows, **self._shape)
+            self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=page_table.device)
+
+    def _kw(self, n_rows: int):
+        return dict(self._shape, n_rows=n_rows, stream=torch.cuda.current_stream().cuda_stream)
+
+    def write(self, k, v, row_ptr=None):
+        """k, v [rows, Hkv, d]: the last tokens of the sequences (row_ptr: first row of each; None: one each) into their pages."""
+        B.cache_write(k, v, self.cache, self.page_table, self.lens, row_ptr, **self._kw(k.shape[0]))
+
+    def read(self, k, v, row_ptr=None):
+        """The last tokens of the sequences from their pages -> k, v."""
+        B.cache_read(self.cache, self.page_table, self.lens, k, v, row_ptr, **self._kw(k.shape[0]))
+
+    def attend(self, q, o, lse, scale, row_ptr=None):
+        """q [rows, Hq, d], the queries of the sequences' last tokens, over their pages -> o, lse [Hq, rows] (or None)."""
+        B.cache_attn(q, self.cache, self.page_table, self.lens, o, lse, self.workspace, row_ptr, n_q_heads=self.n_q_heads, scale=scale,
+                     **self._kw(q.shape[0]))
