@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from functools import lru_cache
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -495,79 +496,97 @@ def bwd_dkdv_plan(tables: Tables, n_q_heads: int, n_kv_heads: int, head_dim: int
     return tuple(int(x) for x in plan)
 
 
-def _check_tensor(t, dtype: str, numel: int, what: str) -> None:
-    """A torch tensor that a kernel will take as `numel` elements of `dtype`, on the current device."""
-    if str(t.dtype) != "torch." + dtype:
-        raise ValueError(f"{what}: {t.dtype}, expected torch.{dtype}")
-    if t.numel() < numel:
-        raise ValueError(f"{what}: {t.numel()} elements, expected {numel}")
-    if not t.is_cuda or t.device.index != _current_device():
-        raise ValueError(f"{what}: on {t.device}, expected the current GPU")
+@lru_cache(maxsize=None)
+def _torch():
+    import torch
+    return torch
+
+
+@lru_cache(maxsize=None)
+def _torch_dtype(dtype):
+    """The torch type of a library type (None if there is none, which the library refuses)."""
+    return {F32: _torch().float32, BF16: _torch().bfloat16, "int32": _torch().int32, "uint8": _torch().uint8}.get(dtype)
 
 
 def _current_device() -> int:
-    import torch
-    return torch.cuda.current_device()
+    """Index of the current GPU; -2 (no tensor's) where the program has not used one."""
+    cuda = _torch().cuda
+    return cuda.current_device() if cuda.is_initialized() else -2
 
 
-_TORCH_DTYPE = {F32: "float32", BF16: "bfloat16"}
-
-
-def _opt_ptr(t, dtype: str, numel: int, what: str):
-    """_ptr of a contiguous tensor of at least `numel` elements, a raw address, or None."""
-    if t is None or isinstance(t, int):
+def _tensor_ptr(t, dtype, numel: int, what: str, dev: int):
+    """Address of a contiguous torch tensor of at least `numel` elements of `dtype` on the current GPU; a raw address or None as it is."""
+    if t is None or type(t) is int:
         return t
-    _check_tensor(t, dtype, numel, what)
-    return _ptr(t)
+    if t.dtype is not dtype or t.numel() < numel or t.get_device() != dev or not t.is_contiguous():
+        _explain(t, dtype, numel, what, dev)
+    return t.data_ptr()
 
 
-def _rows_ptr(t, T: int, heads: int, d: int, dtype: int, stride: int, what: str):
+def _explain(t, dtype, numel: int, what: str, dev: int) -> None:
+    if t.dtype is not dtype:
+        raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
+    if t.numel() < numel:
+        raise ValueError(f"{what}: {t.numel()} elements, expected {numel}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: on {t.device}, expected the current GPU")
+    raise ValueError(f"{what}: tensor must be contiguous")
+
+
+def _rows_ptr(t, T: int, heads: int, d: int, dtype, stride: int, what: str, dev: int):
     """(address, elements from token to token) of a [T, heads, d] tensor whose heads lie one behind the other (a raw address: `stride`)."""
-    if t is None or isinstance(t, int):
+    if t is None or type(t) is int:
         return t, stride
-    if tuple(t.shape) != (T, heads, d):
+    if t.shape != (T, heads, d):
         raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(T, heads, d)}")
-    _check_tensor(t, _TORCH_DTYPE.get(dtype, str(dtype)), 0, what)
+    if t.dtype is not dtype:
+        raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: on {t.device}, expected the current GPU")
     if T == 0 or heads == 0:
         return t.data_ptr(), 0
-    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+    s = t.stride()
+    if s[2] != 1 or (heads > 1 and s[1] != d):
         raise ValueError(f"{what}: the heads of a token must lie one behind the other")
-    return t.data_ptr(), t.stride(0) if T > 1 else 0
+    return t.data_ptr(), s[0] if T > 1 else 0
 
 
-def _rope_params(T, hq, hkv, d, dtype, rotary_dim, sections, eps, flags) -> _RopeParams:
+def _raise(rc: int, where: str) -> None:
+    if rc != 0:
+        raise SlimAttnError(rc, where, f" hip={load_library().slimattn_last_hip_error()}" if rc == -4 else "")
+
+
+# Parameter structures are kept by their plain values: a program calls with few of them, and filling one costs as much as a launch.
+@lru_cache(maxsize=512)
+def _rope_params(T, hq, hkv, d, dtype, rotary_dim, sections, eps, flags, q_stride=0, k_stride=0, dq_stride=0, dk_stride=0):
+    """(structure, its workspace bytes)."""
     p = _RopeParams(total_tokens=T, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, dtype=dtype, rotary_dim=rotary_dim, n_axes=len(sections),
-                    eps=eps, flags=flags)
+                    eps=eps, flags=flags, q_stride=q_stride, k_stride=k_stride, dq_stride=dq_stride, dk_stride=dk_stride)
     if len(sections) <= 4:                                      # (the library refuses more axes)
         p.sections = (C.c_int32 * 4)(*sections)
-    return p
-
-
-def _rope_small(q_weight, k_weight, positions, inv_freq, T, d, rotary_dim, n_axes):
-    return (_opt_ptr(q_weight, "float32", d, "q_weight"), _opt_ptr(k_weight, "float32", d, "k_weight"),
-            _opt_ptr(positions, "int32", n_axes * T, "positions"), _opt_ptr(inv_freq, "float32", rotary_dim // 2, "inv_freq"))
+    return p, int(load_library().slimattn_rope_bwd_workspace_bytes(C.byref(p)))
 
 
 def rope_fwd(q, k, positions, inv_freq, q_out, k_out, *, total_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int,
              rotary_dim: int, sections: Sequence[int], q_weight=None, k_weight=None, eps: float = 1e-6, flags: int = 0, q_stride: int = 0,
              k_stride: int = 0, stream: Optional[int] = None) -> None:
     """slimattn_rope_fwd: q, k [T, heads, d] (rows any distance apart, for raw addresses q_stride, k_stride) -> q_out, k_out packed."""
-    lib = load_library()
-    p = _rope_params(total_tokens, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, sections, eps, flags)
-    dims = (total_tokens, head_dim, dtype)
-    pq, p.q_stride = _rows_ptr(q, dims[0], n_q_heads, *dims[1:], q_stride, "q")
-    pk, p.k_stride = _rows_ptr(k, dims[0], n_kv_heads, *dims[1:], k_stride, "k")
-    n = total_tokens * head_dim
-    rc = lib.slimattn_rope_fwd(C.byref(p), pq, pk, *_rope_small(q_weight, k_weight, positions, inv_freq, total_tokens, head_dim, rotary_dim, len(sections)),
-                               _opt_ptr(q_out, _TORCH_DTYPE.get(dtype), n * n_q_heads, "q_out"),
-                               _opt_ptr(k_out, _TORCH_DTYPE.get(dtype), n * n_kv_heads, "k_out"), stream)
+    lib = _lib or load_library()
+    T, d, td, f32, dev = total_tokens, head_dim, _torch_dtype(dtype), _torch_dtype(F32), _current_device()
+    pq, q_stride = _rows_ptr(q, T, n_q_heads, d, td, q_stride, "q", dev)
+    pk, k_stride = _rows_ptr(k, T, n_kv_heads, d, td, k_stride, "k", dev)
+    sections = tuple(sections)
+    p, _ = _rope_params(T, n_q_heads, n_kv_heads, d, dtype, rotary_dim, sections, eps, flags, q_stride, k_stride)
+    rc = lib.slimattn_rope_fwd(p, pq, pk, _tensor_ptr(q_weight, f32, d, "q_weight", dev), _tensor_ptr(k_weight, f32, d, "k_weight", dev),
+                               _tensor_ptr(positions, _torch_dtype("int32"), len(sections) * T, "positions", dev),
+                               _tensor_ptr(inv_freq, f32, rotary_dim // 2, "inv_freq", dev), _tensor_ptr(q_out, td, T * d * n_q_heads, "q_out", dev),
+                               _tensor_ptr(k_out, td, T * d * n_kv_heads, "k_out", dev), stream)
     _raise(rc, "slimattn_rope_fwd")
 
 
 def rope_bwd_workspace_bytes(total_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, rotary_dim: int,
                              sections: Sequence[int], eps: float = 1e-6, flags: int = 0) -> int:
-    p = _rope_params(total_tokens, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, sections, eps, flags)
-    return int(load_library().slimattn_rope_bwd_workspace_bytes(C.byref(p)))
+    return _rope_params(total_tokens, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, tuple(sections), eps, flags)[1]
 
 
 def rope_bwd(q, k, positions, inv_freq, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, *, total_tokens: int, n_q_heads: int,
@@ -575,24 +594,35 @@ def rope_bwd(q, k, positions, inv_freq, dq_out, dk_out, dq, dk, dq_weight, dk_we
              eps: float = 1e-6, flags: int = 0, q_stride: int = 0, k_stride: int = 0, dq_stride: int = 0, dk_stride: int = 0,
              stream: Optional[int] = None) -> None:
     """slimattn_rope_bwd: dq_out, dk_out packed -> dq, dk (rows any distance apart) and, with ROPE_NORM, dq_weight, dk_weight."""
-    lib = load_library()
-    p = _rope_params(total_tokens, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, sections, eps, flags)
-    T, d = total_tokens, head_dim
-    pq, p.q_stride = _rows_ptr(q, T, n_q_heads, d, dtype, q_stride, "q")
-    pk, p.k_stride = _rows_ptr(k, T, n_kv_heads, d, dtype, k_stride, "k")
-    pdq, p.dq_stride = _rows_ptr(dq, T, n_q_heads, d, dtype, dq_stride, "dq")
-    pdk, p.dk_stride = _rows_ptr(dk, T, n_kv_heads, d, dtype, dk_stride, "dk")
-    need = int(lib.slimattn_rope_bwd_workspace_bytes(C.byref(p))) if dq_weight is not None or dk_weight is not None else 0
-    rc = lib.slimattn_rope_bwd(C.byref(p), pq, pk, *_rope_small(q_weight, k_weight, positions, inv_freq, T, d, rotary_dim, len(sections)),
-                               _opt_ptr(dq_out, _TORCH_DTYPE.get(dtype), T * d * n_q_heads, "dq_out"),
-                               _opt_ptr(dk_out, _TORCH_DTYPE.get(dtype), T * d * n_kv_heads, "dk_out"), pdq, pdk,
-                               _opt_ptr(dq_weight, "float32", d, "dq_weight"), _opt_ptr(dk_weight, "float32", d, "dk_weight"),
-                               _opt_ptr(workspace, "uint8", need, "workspace"), stream)
+    lib = _lib or load_library()
+    T, d, td, f32, dev = total_tokens, head_dim, _torch_dtype(dtype), _torch_dtype(F32), _current_device()
+    pq, q_stride = _rows_ptr(q, T, n_q_heads, d, td, q_stride, "q", dev)
+    pk, k_stride = _rows_ptr(k, T, n_kv_heads, d, td, k_stride, "k", dev)
+    pdq, dq_stride = _rows_ptr(dq, T, n_q_heads, d, td, dq_stride, "dq", dev)
+    pdk, dk_stride = _rows_ptr(dk, T, n_kv_heads, d, td, dk_stride, "dk", dev)
+    sections = tuple(sections)
+    p, need = _rope_params(T, n_q_heads, n_kv_heads, d, dtype, rotary_dim, sections, eps, flags, q_stride, k_stride, dq_stride, dk_stride)
+    if dq_weight is None and dk_weight is None:
+        need = 0
+    rc = lib.slimattn_rope_bwd(p, pq, pk, _tensor_ptr(q_weight, f32, d, "q_weight", dev), _tensor_ptr(k_weight, f32, d, "k_weight", dev),
+                               _tensor_ptr(positions, _torch_dtype("int32"), len(sections) * T, "positions", dev),
+                               _tensor_ptr(inv_freq, f32, rotary_dim // 2, "inv_freq", dev), _tensor_ptr(dq_out, td, T * d * n_q_heads, "dq_out", dev),
+                               _tensor_ptr(dk_out, td, T * d * n_kv_heads, "dk_out", dev), pdq, pdk, _tensor_ptr(dq_weight, f32, d, "dq_weight", dev),
+                               _tensor_ptr(dk_weight, f32, d, "dk_weight", dev), _tensor_ptr(workspace, _torch_dtype("uint8"), need, "workspace", dev),
+                               stream)
     _raise(rc, "slimattn_rope_bwd")
 
 
-def _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows) -> _CacheParams:
-    return _CacheParams(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+@lru_cache(maxsize=512)
+def _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows):
+    """(structure, bytes of the cache)."""
+    return (_CacheParams(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows),
+            cache_bytes(n_pages, page_size, n_kv_heads, head_dim))
+
+
+@lru_cache(maxsize=512)
+def _cache_attn_bytes(n_q_heads, *shape):
+    return int(load_library().slimattn_cache_attn_workspace_bytes(_cache_params(*shape)[0], n_q_heads))
 
 
 def cache_bytes(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int) -> int:
@@ -600,55 +630,51 @@ def cache_bytes(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int) ->
     return int(load_library().slimattn_cache_bytes(n_pages, page_size, n_kv_heads, head_dim))
 
 
-def _cache_arrays(p: _CacheParams, cache, page_table, lens, row_ptr):
+def _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev):
     """Addresses (row_ptr, lens, page_table, cache), the tensors among them checked."""
-    return (_opt_ptr(row_ptr, "int32", p.n_seqs + 1, "row_ptr"), _opt_ptr(lens, "int32", p.n_seqs, "lens"),
-            _opt_ptr(page_table, "int32", p.n_seqs * p.max_pages, "page_table"),
-            _opt_ptr(cache, "uint8", 0 if isinstance(cache, int) else cache_bytes(p.n_pages, p.page_size, p.n_kv_heads, p.head_dim), "cache"))
+    i32 = _torch_dtype("int32")
+    return (_tensor_ptr(row_ptr, i32, p.n_seqs + 1, "row_ptr", dev), _tensor_ptr(lens, i32, p.n_seqs, "lens", dev),
+            _tensor_ptr(page_table, i32, p.n_seqs * p.max_pages, "page_table", dev), _tensor_ptr(cache, _torch_dtype("uint8"), size, "cache", dev))
 
 
 def cache_write(k, v, cache, page_table, lens, row_ptr=None, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
                 dtype: int, n_seqs: int, max_pages: int, k_stride: int = 0, v_stride: int = 0, stream: Optional[int] = None) -> None:
     """slimattn_cache_write: k, v [n_rows, Hkv, d] (rows any distance apart, for raw addresses k_stride, v_stride) into the cache."""
-    p = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
-    pk, k_stride = _rows_ptr(k, n_rows, n_kv_heads, head_dim, dtype, k_stride, "k")
-    pv, v_stride = _rows_ptr(v, n_rows, n_kv_heads, head_dim, dtype, v_stride, "v")
-    rp, ln, pt, ca = _cache_arrays(p, cache, page_table, lens, row_ptr)
-    _raise(load_library().slimattn_cache_write(C.byref(p), pk, pv, k_stride, v_stride, rp, ln, pt, ca, stream), "slimattn_cache_write")
+    lib, td, dev = _lib or load_library(), _torch_dtype(dtype), _current_device()
+    p, size = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+    pk, k_stride = _rows_ptr(k, n_rows, n_kv_heads, head_dim, td, k_stride, "k", dev)
+    pv, v_stride = _rows_ptr(v, n_rows, n_kv_heads, head_dim, td, v_stride, "v", dev)
+    rp, ln, pt, ca = _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev)
+    _raise(lib.slimattn_cache_write(p, pk, pv, k_stride, v_stride, rp, ln, pt, ca, stream), "slimattn_cache_write")
 
 
 def cache_read(cache, page_table, lens, k, v, row_ptr=None, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
                dtype: int, n_seqs: int, max_pages: int, stream: Optional[int] = None) -> None:
     """slimattn_cache_read: the cache's values of the rows -> k, v [n_rows, Hkv, d] packed."""
-    p = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
-    rp, ln, pt, ca = _cache_arrays(p, cache, page_table, lens, row_ptr)
-    n, name = n_rows * n_kv_heads * head_dim, _TORCH_DTYPE.get(dtype)
-    _raise(load_library().slimattn_cache_read(C.byref(p), ca, rp, ln, pt, _opt_ptr(k, name, n, "k"), _opt_ptr(v, name, n, "v"), stream),
-           "slimattn_cache_read")
+    lib, td, dev = _lib or load_library(), _torch_dtype(dtype), _current_device()
+    p, size = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+    rp, ln, pt, ca = _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev)
+    n = n_rows * n_kv_heads * head_dim
+    _raise(lib.slimattn_cache_read(p, ca, rp, ln, pt, _tensor_ptr(k, td, n, "k", dev), _tensor_ptr(v, td, n, "v", dev), stream), "slimattn_cache_read")
 
 
 def cache_attn_workspace_bytes(n_q_heads: int, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: int,
                                n_seqs: int, max_pages: int) -> int:
-    p = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
-    return int(load_library().slimattn_cache_attn_workspace_bytes(C.byref(p), n_q_heads))
+    return _cache_attn_bytes(n_q_heads, n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
 
 
 def cache_attn(q, cache, page_table, lens, o, lse, workspace, row_ptr=None, *, n_q_heads: int, scale: float, n_rows: int, n_pages: int,
                page_size: int, n_kv_heads: int, head_dim: int, dtype: int, n_seqs: int, max_pages: int, stream: Optional[int] = None) -> None:
     """slimattn_cache_attn: q [n_rows, Hq, d] over the cache -> o, and lse [Hq, n_rows] unless it is None."""
-    lib = load_library()
-    p = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
-    rp, ln, pt, ca = _cache_arrays(p, cache, page_table, lens, row_ptr)
-    n, name = n_rows * n_q_heads * head_dim, _TORCH_DTYPE.get(dtype)
-    need = int(lib.slimattn_cache_attn_workspace_bytes(C.byref(p), n_q_heads))
-    rc = lib.slimattn_cache_attn(C.byref(p), n_q_heads, scale, _opt_ptr(q, name, n, "q"), rp, ln, pt, ca, _opt_ptr(o, name, n, "o"),
-                                 _opt_ptr(lse, "float32", n_rows * n_q_heads, "lse"), _opt_ptr(workspace, "uint8", need, "workspace"), stream)
+    lib, td, dev = _lib or load_library(), _torch_dtype(dtype), _current_device()
+    shape = (n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+    p, size = _cache_params(*shape)
+    rp, ln, pt, ca = _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev)
+    n = n_rows * n_q_heads * head_dim
+    rc = lib.slimattn_cache_attn(p, n_q_heads, scale, _tensor_ptr(q, td, n, "q", dev), rp, ln, pt, ca, _tensor_ptr(o, td, n, "o", dev),
+                                 _tensor_ptr(lse, _torch_dtype(F32), n_rows * n_q_heads, "lse", dev),
+                                 _tensor_ptr(workspace, _torch_dtype("uint8"), _cache_attn_bytes(n_q_heads, *shape), "workspace", dev), stream)
     _raise(rc, "slimattn_cache_attn")
-
-
-def _raise(rc: int, where: str) -> None:
-    if rc != 0:
-        raise SlimAttnError(rc, where, f" hip={load_library().slimattn_last_hip_error()}" if rc == -4 else "")
 
 
 STATIC_SCRATCH_BYTES = 64 << 20

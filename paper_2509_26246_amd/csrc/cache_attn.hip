@@ -28,7 +28,7 @@ constexpr int kCols = 16;            // query columns of a tile
 constexpr int kStep = 64;            // keys of a wave's step
 constexpr int kUnit = kWaves * kStep;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kMaxGrid = 1024;       // four blocks per compute unit
+constexpr int kMaxGrid = 1024;       // at most four blocks per compute unit
 
 struct AttnArgs {
   CacheView c;
@@ -51,11 +51,12 @@ __device__ __forceinline__ float* part_of(char* ws, int block, int slot) {
 typedef float floatx4v __attribute__((ext_vector_type(4)));
 typedef int int2v __attribute__((ext_vector_type(2)));
 template <int D> struct Piece;                    // what a lane loads of D/2 bytes x 16 keys, or of the scales
-template <> struct Piece<128> { typedef uint4 type; };
-template <> struct Piece<64> { typedef uint2 type; };
+template <> struct Piece<128> { typedef uint4 type; typedef uint2 scale; };
+template <> struct Piece<64> { typedef uint2 type; typedef unsigned scale; };
 
 __device__ __forceinline__ unsigned word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ unsigned word(const uint2& v, int i) { return i == 0 ? v.x : v.y; }
+__device__ __forceinline__ unsigned word(unsigned v, int) { return v; }
 
 __device__ __forceinline__ floatx4v mfma16(bf16x8 a, bf16x8 b, floatx4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -76,43 +77,70 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&t)[TER
     }
 }
 
-// LDS of one wave: V codes (rows of D/2 bytes, 16 more to spread the transpose reads over the banks), K scales, V scales.
+// LDS of one wave: V codes, rows of D/2 bytes and 16 more (the transpose reads take the same 8 bytes of 16 rows at once).
 template <int D> constexpr int kVRow = D / 2 + 16;
-template <int D> constexpr int kScaleBytes = kStep * (D / 16);
-template <int D> constexpr int kWaveLds = kStep * kVRow<D> + 2 * kScaleBytes<D>;
+template <int D> constexpr int kWaveLds = kStep * kVRow<D>;
 template <int D> constexpr int kOutRow = D + 4;                                    // floats; at the end: [wave][col][kOutRow], max, sum
 template <int D> constexpr int kEndLds = kWaves * kCols * (kOutRow<D> + 2) * 4;
 template <int D> constexpr int kLds = kWaves * kWaveLds<D> > kEndLds<D> ? kWaves * kWaveLds<D> : kEndLds<D>;
 
-// One step's loads.
+// Waves per SIMD, by what their registers take (bf16 158 and 114 of them at head dim 128 and 64, f32 213 and 150): nothing is spilled.
+template <int D, int TERMS> constexpr int kBlocksPerCu = TERMS == 1 ? (D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
+
+// One step's loads.  Tile t of the score product is the step's t-th chunk of 16 keys, so its C layout gives lane group h = lane / 16 the
+// keys 16t + 4h + i (t, i = 0..3): "its" key number e = 4t + i of 16.  A lane's own key, whose scales it holds, is number lane % 16.
 template <int D>
 struct StepData {
   typedef typename Piece<D>::type P;
-  P k[4], v[4], s;
-  unsigned ok;                       // bit h: the keys 16h .. 16h+15 are in a page (uniform)
+  typedef typename Piece<D>::scale S;
+  P k[4], v[4];
+  S ks, vs;
 };
 
+// The table's entry for this lane's own key (pages of the step's chunk t: lanes with (lane >> 2) % 4 = t), to be checked by step_pages.
+__device__ __forceinline__ int load_page(const CacheView& c, const int32_t* table, int k0, int end) {
+  const int key = k0 + kCacheChunk * ((threadIdx.x >> 2) & 3);
+  const int page = table[min(key, end - 1) >> c.page_shift];   // (no branch in the loop: the last steps look up and load what they drop)
+  return key < end ? page : -1;
+}
+// Bit t: the chunk is in a page.  Chunks without one take page 0 and are masked.
+__device__ __forceinline__ unsigned step_pages(const CacheView& c, int& page) {
+  const bool there = (unsigned)page < (unsigned)c.n_pages;
+  page = there ? page : 0;
+  const unsigned good = (unsigned)__ballot(there);
+  return (good & 1) | (good >> 3 & 2) | (good >> 6 & 4) | (good >> 9 & 8);
+}
+
 template <int D>
-__device__ __forceinline__ void load_step(StepData<D>& x, const CacheView& c, const char* cache, int b, int hk, int k0, int visible) {
-  typedef typename Piece<D>::type P;
-  const int lane = threadIdx.x & 63, P_mask = (1 << c.page_shift) - 1;
-  const int chunk = (lane >> 2) & 3, key = k0 + kCacheChunk * chunk;
-  int page = key < visible ? page_at(c, b, key) : -1;
-  const unsigned long long good = __ballot(page >= 0);
-  x.ok = (unsigned)(good & 1) | (unsigned)((good >> 4 & 1) << 1) | (unsigned)((good >> 8 & 1) << 2) | (unsigned)((good >> 12 & 1) << 3);
-  page = max(page, 0);               // chunks without a page read page 0 and are masked
-  const long long piece = hk * head_bytes<D>(c), pb = page_bytes<D>(c);
-  const char* kp = cache + page * pb + piece + key_codes<D>((key & P_mask) + (lane & 3)) + (lane >> 4) * (D / 8);
+__device__ __forceinline__ void load_values(StepData<D>& x, const CacheView& c, const char* head, unsigned pb, int page, int k0) {
+  typedef typename StepData<D>::P P;
+  const int lane = threadIdx.x & 63, in_page = (1 << c.page_shift) - 1;
 #pragma unroll
-  for (int t = 0; t < 4; ++t) x.k[t] = *reinterpret_cast<const P*>(kp + 4 * t * (D / 2));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int pi = __builtin_amdgcn_readlane(page, 4 * i);
-    x.v[i] = *reinterpret_cast<const P*>(cache + pi * pb + piece + value_codes<D>(c, (k0 + kCacheChunk * i) & P_mask) + lane * (int)sizeof(P));
+  for (int t = 0; t < 4; ++t) {
+    const char* base = head + (size_t)(unsigned)__builtin_amdgcn_readlane(page, 4 * t) * pb + value_codes<D>(c, (k0 + kCacheChunk * t) & in_page);
+    x.v[t] = *reinterpret_cast<const P*>(base + lane * (int)sizeof(P));
   }
-  const int sc = (lane >> 3) & 3;
-  const int ps = __shfl(page, 4 * sc);
-  x.s = *reinterpret_cast<const P*>(cache + ps * pb + piece + scales<D>(c, lane >> 5, (k0 + kCacheChunk * sc) & P_mask) + (lane & 7) * (int)sizeof(P));
+}
+template <int D>
+__device__ __forceinline__ void load_keys(StepData<D>& x, const CacheView& c, const char* head, unsigned pb, int page, int k0) {
+  typedef typename StepData<D>::P P;
+  typedef typename StepData<D>::S S;
+  const int lane = threadIdx.x & 63, in_page = (1 << c.page_shift) - 1;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const char* base = head + (size_t)(unsigned)__builtin_amdgcn_readlane(page, 4 * t) * pb + key_codes<D>((k0 + kCacheChunk * t) & in_page);
+    x.k[t] = *reinterpret_cast<const P*>(base + (lane & 15) * (D / 2) + (lane >> 4) * (D / 8));
+  }
+  const int own = k0 + kCacheChunk * ((lane >> 2) & 3) + 4 * (lane >> 4) + (lane & 3);
+  const char* sp = head + (size_t)(unsigned)page * pb + scales<D>(c, 0, own & in_page);
+  x.ks = *reinterpret_cast<const S*>(sp);
+  x.vs = *reinterpret_cast<const S*>(sp + ((D / 16) << c.page_shift));
+}
+
+// Value of lane e of each group of 16.
+template <int E>
+__device__ __forceinline__ float from_lane(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x150 + E, 0xf, 0xf, true));
 }
 
 // The running state of a wave's 16 columns: column lane % 16, and of O^T channels 16 ct + 4h + i.
@@ -122,44 +150,70 @@ struct State {
   float m, l;
 };
 
-// limit: the column's position (its last visible key); unmasked steps are visible to all columns that are rows (the others, q = 0, may
-// come to anything: they are dropped).
-template <int D, int TERMS, bool MASKED>
-__device__ __forceinline__ void step(State<D>& st, const StepData<D>& x, const bf16x8 (&q)[D / 32][TERMS], const char* lds, int k0, int limit,
-                                     float scale_log2) {
-  constexpr int G = D / 32;
-  const int lane = threadIdx.x & 63, h = lane >> 4;
-  float s[16];
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    // scales of keys 16h + 4t .. +3: G per key
-    unsigned sw[2 * G];
-    const char* sp = lds + kStep * kVRow<D> + (16 * h + 4 * t) * (D / 16);
-#pragma unroll
-    for (int i = 0; i < 2 * G; i += 4) {
-      const uint4 w = *reinterpret_cast<const uint4*>(sp + 4 * i);
-      sw[i] = w.x; sw[i + 1] = w.y; sw[i + 2] = w.z; sw[i + 3] = w.w;
-    }
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
+// Scores of the step's 64 keys, in units of `scale`.
+template <int D, int TERMS>
+__device__ __forceinline__ void score_step(float (&s)[16], const StepData<D>& x, const float (&ks)[D / 32], const bf16x8 (&q)[D / 32][TERMS]) {
+  static_for<0, 4>([&](auto t_) {
+    constexpr int t = decltype(t_)::value;
+    static_for<0, D / 32>([&](auto g_) {
+      constexpr int g = decltype(g_)::value;
       const bf16x8 a = codes_to_bf16(word(x.k[t], g));
       floatx4v p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int n = TERMS - 1; n >= 0; --n) p = mfma16(a, q[g][n], p);
+      static_for<0, 4>([&](auto i_) {
+        constexpr int e = 4 * t + decltype(i_)::value;
+        const float f = from_lane<e>(ks[g]);
+        s[e] = g == 0 ? p[e & 3] * f : __builtin_fmaf(p[e & 3], f, s[e]);
+      });
+    });
+    // one tile's products at a time: all at once do not fit the registers
+    asm volatile("" : "+v"(s[4 * t]), "+v"(s[4 * t + 1]), "+v"(s[4 * t + 2]), "+v"(s[4 * t + 3]));
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
+// Scores of keys that a column does not see.  limit: the column's position (its last visible key); there: step_pages.
+__device__ __forceinline__ void mask_step(float (&s)[16], int k0, int limit, unsigned there) {
+  const int last = limit - k0 - 4 * (int)((threadIdx.x & 63) >> 4);
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+    if (16 * (e >> 2) + (e & 3) > last || !(there >> (e >> 2) & 1)) s[e] = -INFINITY;
+}
+
+// A masked step's value scales may be anything (keys behind the end) or rightly NaN for some columns only.  Products with a probability of 0
+// must not see them: scales that are not finite become 0, and columns that do see the key get their NaN here.
+template <int D>
+__device__ __forceinline__ void clean_scales(State<D>& st, const float (&s)[16], float (&vs)[D / 32]) {
+  static_for<0, D / 32>([&](auto g_) {
+    constexpr int g = decltype(g_)::value;
+    const bool bad = !(vs[g] - vs[g] == 0.f);
+    if (__any(bad)) {
+      bool hit = false;
+      static_for<0, 16>([&](auto e_) {
+        constexpr int e = decltype(e_)::value;
+        const float f = from_lane<e>(vs[g]);
+        hit |= !(f - f == 0.f) && s[e] != 0.f;
+      });
+      hit |= (bool)__shfl_xor((int)hit, 16);                 // the column's other lane groups hold other channels
+      hit |= (bool)__shfl_xor((int)hit, 32);
+      const float poison = hit ? __builtin_nanf("") : 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const unsigned w = sw[i * (G / 2) + g / 2];
-        const float f = g & 1 ? hi_bf16(w) : lo_bf16(w);
-        s[4 * t + i] = g == 0 ? p[i] * f : __builtin_fmaf(p[i], f, s[4 * t + i]);
+        st.o[2 * g][i] += poison;
+        st.o[2 * g + 1][i] += poison;
       }
+      vs[g] = bad ? 0.f : vs[g];
     }
-  }
-  if (MASKED) {
-    const int last = x.ok >> h & 1 ? limit - k0 - 16 * h : -1;
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (e > last) s[e] = -INFINITY;
-  }
+  });
+}
+
+// masked: the step has keys that some column does not see (uniform).  (Columns that are no rows, q = 0, may come to anything: they are dropped.)
+template <int D, int TERMS>
+__device__ __forceinline__ void softmax_step(State<D>& st, float (&s)[16], float (&vs)[D / 32], const char* vp, bool masked, int k0, int limit,
+                                             unsigned there, float scale_log2) {
+  constexpr int G = D / 32;
+  if (masked) mask_step(s, k0, limit, there);
   float mx = s[0];
 #pragma unroll
   for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
@@ -179,37 +233,29 @@ __device__ __forceinline__ void step(State<D>& st, const StepData<D>& x, const b
     s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale_log2, -m));
     st.l += s[e];
   }
-  const char* vs = lds + kStep * kVRow<D> + kScaleBytes<D> + 16 * h * (D / 16);
-  const char* vp = lds + lane * kVRow<D>;                    // row 16h + lane % 16 for the transpose reads
+  if (masked) clean_scales<D>(st, s, vs);
+  static_for<0, G>([&](auto g_) {
+    constexpr int g = decltype(g_)::value;
+    float p[2][8];
+    static_for<0, 16>([&](auto e_) {
+      constexpr int e = decltype(e_)::value;
+      p[e >> 3][e & 7] = s[e] * from_lane<e>(vs[g]);
+    });
+    bf16x8 pt[2][TERMS];
+    split_terms<TERMS>(p[0], pt[0]);
+    split_terms<TERMS>(p[1], pt[1]);
 #pragma unroll
-  for (int gp = 0; gp < G / 2; ++gp) {                       // two scale groups share a word
-    unsigned sw[16];
+    for (int ct = 2 * g; ct < 2 * g + 2; ++ct) {
+      const int2v w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((LDS_PTR(int2v))(vp + 8 * ct));
+      const bf16x8 a0 = codes_to_bf16((unsigned)w.x), a1 = codes_to_bf16((unsigned)w.y);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sw[e] = *reinterpret_cast<const unsigned*>(vs + e * (D / 16) + 4 * gp);
-#pragma unroll
-    for (int gi = 0; gi < 2; ++gi) {
-      float p[2][8];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float f = gi ? hi_bf16(sw[e]) : lo_bf16(sw[e]);
-        p[e >> 3][e & 7] = MASKED && s[e] == 0.f ? 0.f : s[e] * f;   // (a masked key's scale may be anything)
-      }
-      bf16x8 pt[2][TERMS];
-      split_terms<TERMS>(p[0], pt[0]);
-      split_terms<TERMS>(p[1], pt[1]);
-#pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2) {
-        const int ct = 4 * gp + 2 * gi + c2;
-        const int2v w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((LDS_PTR(int2v))(vp + 8 * ct));
-        const bf16x8 a0 = codes_to_bf16((unsigned)w.x), a1 = codes_to_bf16((unsigned)w.y);
-#pragma unroll
-        for (int n = TERMS - 1; n >= 0; --n) {
-          st.o[ct] = mfma16(a0, pt[0][n], st.o[ct]);
-          st.o[ct] = mfma16(a1, pt[1][n], st.o[ct]);
-        }
+      for (int n = TERMS - 1; n >= 0; --n) {
+        st.o[ct] = mfma16(a0, pt[0][n], st.o[ct]);
+        st.o[ct] = mfma16(a1, pt[1][n], st.o[ct]);
       }
     }
-  }
+    __builtin_amdgcn_sched_barrier(0);
+  });
 }
 
 // What a sequence contributes to the row of units: its rows, tiles, units per tile.
@@ -281,7 +327,7 @@ __device__ __forceinline__ void store_out(float* p, const float (&x)[N]) {
 }
 
 template <class T, int D, int TERMS>
-__global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(AttnArgs a, const T* __restrict__ q, const char* __restrict__ cache,
+__global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn_kernel(AttnArgs a, const T* __restrict__ q, const char* __restrict__ cache,
                                                                  T* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws) {
   typedef typename Piece<D>::type P;
   __shared__ __align__(16) char lds[kLds<D>];
@@ -352,29 +398,58 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(AttnArgs a, con
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct) st.o[ct] = floatx4v{0.f, 0.f, 0.f, 0.f};
 
-    char* mine_lds = lds + wave * kWaveLds<D>;
+    char* vrows = lds + wave * kWaveLds<D>;
+    const char* vp = vrows + lane * kVRow<D>;                // the rows of the lane group's 16 keys, in their order
+    char* vw;                                                // where the lane's piece of chunk 0 goes; the next chunks 4 rows further each
+    {
+      const int at = lane * (int)sizeof(P), r = at / (D / 2);
+      vw = vrows + (16 * (r >> 2) + (r & 3)) * kVRow<D> + at % (D / 2);
+    }
     const int end = min(last * kUnit, visible);
+    const int32_t* table = a.c.table + (size_t)b * a.c.max_pages;
+    const char* head_piece = cache + hk * head_bytes<D>(a.c);
+    const unsigned pb = (unsigned)page_bytes<D>(a.c);
     int k0 = first * kUnit + wave * kStep;
     StepData<D> x;
-    if (k0 < end) load_step<D>(x, a.c, cache, b, hk, k0, visible);
+    unsigned there = 0;
+    int page = -1;
+    if (k0 < end) {
+      page = load_page(a.c, table, k0, end);
+      const int after = load_page(a.c, table, k0 + kUnit, end);
+      there = step_pages(a.c, page);
+      load_values<D>(x, a.c, head_piece, pb, page, k0);
+      load_keys<D>(x, a.c, head_piece, pb, page, k0);
+      page = after;
+    }
     for (; k0 < end; k0 += kUnit) {
+      // this step's values into LDS, its scales into registers; then the next step's are on their way
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = lane * (int)sizeof(P);                // 16 keys of D/2 bytes
-        *reinterpret_cast<P*>(mine_lds + (16 * i + at / (D / 2)) * kVRow<D> + at % (D / 2)) = x.v[i];
+      for (int t = 0; t < 4; ++t) *reinterpret_cast<P*>(vw + 4 * t * kVRow<D>) = x.v[t];
+      float ks[D / 32], vs[D / 32];
+#pragma unroll
+      for (int g = 0; g < D / 32; ++g) {
+        ks[g] = g & 1 ? hi_bf16(word(x.ks, g / 2)) : lo_bf16(word(x.ks, g / 2));
+        vs[g] = g & 1 ? hi_bf16(word(x.vs, g / 2)) : lo_bf16(word(x.vs, g / 2));
       }
-      *reinterpret_cast<P*>(mine_lds + kStep * kVRow<D> + (lane >> 5) * kScaleBytes<D> + (lane & 31) * (int)sizeof(P)) = x.s;
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
-      const StepData<D> now = x;
-      if (k0 + kUnit < end) load_step<D>(x, a.c, cache, b, hk, k0 + kUnit, visible);
-      if (now.ok == 15 && k0 + kStep <= all_see) step<D, TERMS, false>(st, now, qf, mine_lds, k0, limit, a.scale_log2);
-      else step<D, TERMS, true>(st, now, qf, mine_lds, k0, limit, a.scale_log2);
+      const unsigned now = there;
+      there = step_pages(a.c, page);
+      load_values<D>(x, a.c, head_piece, pb, page, k0 + kUnit);
+      float s[16];
+      score_step<D, TERMS>(s, x, ks, qf);
+      load_keys<D>(x, a.c, head_piece, pb, page, k0 + kUnit);
+      page = load_page(a.c, table, k0 + 2 * kUnit, end);
+      softmax_step<D, TERMS>(st, s, vs, vp, now != 15 || k0 + kStep > all_see, k0, limit, now, a.scale_log2);
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
     }
 
-    // the four waves' states together
+    // the four waves' states together (from a copy of the thread's number made here: what is derived from it would otherwise be kept in
+    // registers through every walk)
+    int me = tid;
+    asm volatile("" : "+v"(me));
+    const int my_col = me & 15, my_h = me >> 4 & 3;
     st.l += __shfl_xor(st.l, 16);
     st.l += __shfl_xor(st.l, 32);
     __syncthreads();
@@ -382,15 +457,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(AttnArgs a, con
     float* stat = ends + kWaves * kCols * kOutRow<D>;        // [wave][col] maximum, then sum
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct)
-      *reinterpret_cast<floatx4v*>(ends + (wave * kCols + col) * kOutRow<D> + 16 * ct + 4 * h) = st.o[ct];
-    if (h == 0) {
-      stat[wave * kCols + col] = st.m;
-      stat[kWaves * kCols + wave * kCols + col] = st.l;
+      *reinterpret_cast<floatx4v*>(ends + (wave * kCols + my_col) * kOutRow<D> + 16 * ct + 4 * my_h) = st.o[ct];
+    if (my_h == 0) {
+      stat[wave * kCols + my_col] = st.m;
+      stat[kWaves * kCols + wave * kCols + my_col] = st.l;
     }
     __syncthreads();
     {
       constexpr int E = D / 16;                              // channels of a thread
-      const int c = tid >> 4, e0 = (tid & 15) * E;
+      const int c = me >> 4, e0 = (me & 15) * E;
       float m = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[w * kCols + c]);
@@ -481,13 +556,15 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(AttnArgs a, T
   if (lse && e == 0) lse[(size_t)hd * a.c.n_rows + r] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Blocks of the first launch: as many as there can be units, up to four per compute unit.
+// Blocks of the first launch: as many as there can be units, up to what is resident at once.
 int grid_blocks(const slimattn_cache_params& p, int n_q_heads) {
+  const int resident = 256 * (p.dtype == SLIMATTN_BF16 ? (p.head_dim == 128 ? kBlocksPerCu<128, 1> : kBlocksPerCu<64, 1>)
+                                                       : (p.head_dim == 128 ? kBlocksPerCu<128, 3> : kBlocksPerCu<64, 3>));
   const long long cols = (long long)p.n_rows * (n_q_heads / p.n_kv_heads);
   const long long items = (cols / kCols + p.n_seqs) * p.n_kv_heads;
   const long long units = ((long long)p.max_pages * p.page_size + kUnit - 1) / kUnit;
-  const long long most = items > kMaxGrid ? kMaxGrid : items * units;
-  return (int)(most < kMaxGrid ? most : kMaxGrid);
+  const long long most = items > resident ? resident : items * units;
+  return (int)(most < resident ? most : resident);
 }
 
 }  // namespace
