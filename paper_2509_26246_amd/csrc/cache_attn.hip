@@ -35,17 +35,19 @@ struct AttnArgs {
   int group, Hq;                     // query heads per KV head; of all
   float scale_log2;                  // > 0
   float q_sign;                      // scale < 0 turns q around; 0 makes it zero
+  int slots;                         // split items are listed by number if there are at most this many items, 0: by the block that began them
 };
 
-// A split item, written by the block that holds its start, for the launch that adds its parts up.
-struct Split { int first, parts, row0, cols, col0, head0; };
-struct Header { int blocks, pad[7]; };
+// An item that blocks share, written by the one that holds its start for the launch that adds its parts up (parts = 0: not shared).
+struct Split { int first, parts, row0, cols, col0, head0, pad[2]; };
+struct Header { int listed, pad[7]; };   // entries that were written
+__device__ __forceinline__ Split* split_list(char* ws) { return reinterpret_cast<Split*>(ws + sizeof(Header)); }
 
 template <int D> constexpr int kPartFloats = kCols * D + 2 * kCols;   // [col][D], max [col], sum [col]
 
 template <int D>
 __device__ __forceinline__ float* part_of(char* ws, int block, int slot) {
-  return reinterpret_cast<float*>(ws + sizeof(Header) + (size_t)kMaxGrid * 32) + ((size_t)block * 2 + slot) * kPartFloats<D>;
+  return reinterpret_cast<float*>(ws + sizeof(Header) + kMaxGrid * sizeof(Split)) + ((size_t)block * 2 + slot) * kPartFloats<D>;
 }
 
 typedef float floatx4v __attribute__((ext_vector_type(4)));
@@ -97,24 +99,29 @@ struct StepData {
   S ks, vs;
 };
 
-// The table's entry for this lane's own key (pages of the step's chunk t: lanes with (lane >> 2) % 4 = t), to be checked by step_pages.
+// The table's entry for this lane's chunk of a step's keys (chunk t: lanes with (lane >> 2) % 4 = t).  No branch: the last steps look up and
+// load again what they drop.
 __device__ __forceinline__ int load_page(const CacheView& c, const int32_t* table, int k0, int end) {
-  const int key = k0 + kCacheChunk * ((threadIdx.x >> 2) & 3);
-  const int page = table[min(key, end - 1) >> c.page_shift];   // (no branch in the loop: the last steps look up and load what they drop)
-  return key < end ? page : -1;
+  return table[min(k0 + kCacheChunk * (int)((threadIdx.x >> 2) & 3), end - 1) >> c.page_shift];
 }
-// Bit t: the chunk is in a page.  Chunks without one take page 0 and are masked.
-__device__ __forceinline__ unsigned step_pages(const CacheView& c, int& page) {
-  const bool there = (unsigned)page < (unsigned)c.n_pages;
+// Makes a page of it.  Bit t: the chunk is in a page; chunks that are not take page 0 and are masked.
+__device__ __forceinline__ unsigned step_pages(const CacheView& c, int& page, int k0, int end) {
+  const bool there = (unsigned)page < (unsigned)c.n_pages && k0 + kCacheChunk * (int)((threadIdx.x >> 2) & 3) < end;
   page = there ? page : 0;
   const unsigned good = (unsigned)__ballot(there);
   return (good & 1) | (good >> 3 & 2) | (good >> 6 & 4) | (good >> 9 & 8);
 }
 
+// Scales and value codes: needed first.
 template <int D>
 __device__ __forceinline__ void load_values(StepData<D>& x, const CacheView& c, const char* head, unsigned pb, int page, int k0) {
   typedef typename StepData<D>::P P;
+  typedef typename StepData<D>::S S;
   const int lane = threadIdx.x & 63, in_page = (1 << c.page_shift) - 1;
+  const int own = k0 + kCacheChunk * ((lane >> 2) & 3) + 4 * (lane >> 4) + (lane & 3);
+  const char* sp = head + (size_t)(unsigned)page * pb + scales<D>(c, 0, own & in_page);
+  x.ks = *reinterpret_cast<const S*>(sp);
+  x.vs = *reinterpret_cast<const S*>(sp + ((D / 16) << c.page_shift));
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     const char* base = head + (size_t)(unsigned)__builtin_amdgcn_readlane(page, 4 * t) * pb + value_codes<D>(c, (k0 + kCacheChunk * t) & in_page);
@@ -124,17 +131,12 @@ __device__ __forceinline__ void load_values(StepData<D>& x, const CacheView& c, 
 template <int D>
 __device__ __forceinline__ void load_keys(StepData<D>& x, const CacheView& c, const char* head, unsigned pb, int page, int k0) {
   typedef typename StepData<D>::P P;
-  typedef typename StepData<D>::S S;
   const int lane = threadIdx.x & 63, in_page = (1 << c.page_shift) - 1;
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     const char* base = head + (size_t)(unsigned)__builtin_amdgcn_readlane(page, 4 * t) * pb + key_codes<D>((k0 + kCacheChunk * t) & in_page);
     x.k[t] = *reinterpret_cast<const P*>(base + (lane & 15) * (D / 2) + (lane >> 4) * (D / 8));
   }
-  const int own = k0 + kCacheChunk * ((lane >> 2) & 3) + 4 * (lane >> 4) + (lane & 3);
-  const char* sp = head + (size_t)(unsigned)page * pb + scales<D>(c, 0, own & in_page);
-  x.ks = *reinterpret_cast<const S*>(sp);
-  x.vs = *reinterpret_cast<const S*>(sp + ((D / 16) << c.page_shift));
 }
 
 // Value of lane e of each group of 16.
@@ -150,24 +152,34 @@ struct State {
   float m, l;
 };
 
-// Scores of the step's 64 keys, in units of `scale`.
+// Scores of the step's 64 keys, in units of `scale`: a tile's products run while the one before it is scaled.
 template <int D, int TERMS>
 __device__ __forceinline__ void score_step(float (&s)[16], const StepData<D>& x, const float (&ks)[D / 32], const bf16x8 (&q)[D / 32][TERMS]) {
+  constexpr int G = D / 32;
+  floatx4v p[2][G];
+  auto products = [&](auto t_) {
+    constexpr int t = decltype(t_)::value;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const bf16x8 a = codes_to_bf16(word(x.k[t], g));
+      p[t & 1][g] = floatx4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int n = TERMS - 1; n >= 0; --n) p[t & 1][g] = mfma16(a, q[g][n], p[t & 1][g]);
+    }
+  };
+  products(IC<0>{});
   static_for<0, 4>([&](auto t_) {
     constexpr int t = decltype(t_)::value;
-    static_for<0, D / 32>([&](auto g_) {
-      constexpr int g = decltype(g_)::value;
-      const bf16x8 a = codes_to_bf16(word(x.k[t], g));
-      floatx4v p = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int n = TERMS - 1; n >= 0; --n) p = mfma16(a, q[g][n], p);
-      static_for<0, 4>([&](auto i_) {
-        constexpr int e = 4 * t + decltype(i_)::value;
+    if constexpr (t < 3) products(IC<t + 1>{});
+    static_for<0, 4>([&](auto i_) {
+      constexpr int i = decltype(i_)::value, e = 4 * t + i;
+      static_for<0, G>([&](auto g_) {
+        constexpr int g = decltype(g_)::value;
         const float f = from_lane<e>(ks[g]);
-        s[e] = g == 0 ? p[e & 3] * f : __builtin_fmaf(p[e & 3], f, s[e]);
+        s[e] = g == 0 ? p[t & 1][g][i] * f : __builtin_fmaf(p[t & 1][g][i], f, s[e]);
       });
     });
-    // one tile's products at a time: all at once do not fit the registers
+    // no further ahead: all tiles at once do not fit the registers
     asm volatile("" : "+v"(s[4 * t]), "+v"(s[4 * t + 1]), "+v"(s[4 * t + 2]), "+v"(s[4 * t + 3]));
     __builtin_amdgcn_sched_barrier(0);
   });
@@ -331,42 +343,59 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
                                                                  T* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws) {
   typedef typename Piece<D>::type P;
   __shared__ __align__(16) char lds[kLds<D>];
-  __shared__ long long scan[kWaves], found[2];
+  __shared__ long long scan[kWaves], found[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 4, col = lane & 15;
   const int N = gridDim.x;
   // neighbouring blocks of the row of units on one XCD: tiles of one head read the same keys
   const int id = N % 8 == 0 ? (int)(blockIdx.x % 8) * (N / 8) + blockIdx.x / 8 : blockIdx.x;
 
-  long long U = 0;
+  // the row of units: its length, then the sequence in which this block's first unit lies.  Up to 256 sequences are one look at the lengths.
+  const bool one_look = a.c.n_seqs <= kThreads;
+  long long U = 0, items = 0, mine = 0, my_items = 0;
   for (int b0 = 0; b0 < a.c.n_seqs; b0 += kThreads) {
     const int b = b0 + tid;
-    if (b < a.c.n_seqs) U += seq_units(a, seq_of(a, b));
+    if (b < a.c.n_seqs) {
+      const Seq s = seq_of(a, b);
+      mine += seq_units(a, s);
+      my_items += (long long)s.tiles * a.c.n_kv_heads;
+    }
   }
-  long long mine = U;
-  mine = block_scan(mine, scan, U);
+  const long long units_to = block_scan(mine, scan, U), items_to = a.slots ? block_scan(my_items, scan, items) : 0;
   const int n = (int)min((long long)N, U);                   // blocks with work: no unit, no block
-  if (blockIdx.x == 0 && tid == 0) reinterpret_cast<Header*>(ws)->blocks = n;
+  if (blockIdx.x == 0 && tid == 0) reinterpret_cast<Header*>(ws)->listed = a.slots ? (int)min((long long)a.slots, items) : n;
   if (id >= n) return;
   const long long u0 = U * id / n, u1 = U * (id + 1) / n;
-  long long before = 0;
-  for (int b0 = 0;; b0 += kThreads) {                        // ends: u0 < U
-    const int b = b0 + tid;
-    const long long w = b < a.c.n_seqs ? seq_units(a, seq_of(a, b)) : 0;
-    long long total;
-    const long long end = before + block_scan(w, scan, total);
-    if (u0 < end && u0 >= end - w) { found[0] = b; found[1] = end - w; }
-    if (u0 < before + total) break;
-    before += total;
+  if (one_look) {
+    if (u0 < units_to && u0 >= units_to - mine) { found[0] = tid; found[1] = units_to - mine; found[2] = items_to - my_items; }
+  } else {
+    long long units_before = 0, items_before = 0;
+    for (int b0 = 0;; b0 += kThreads) {                      // ends: u0 < U
+      const int b = b0 + tid;
+      long long w = 0, i = 0, total, total_items = 0;
+      if (b < a.c.n_seqs) {
+        const Seq s = seq_of(a, b);
+        w = seq_units(a, s);
+        i = (long long)s.tiles * a.c.n_kv_heads;
+      }
+      const long long end = units_before + block_scan(w, scan, total);
+      const long long item_end = a.slots ? items_before + block_scan(i, scan, total_items) : 0;
+      if (u0 < end && u0 >= end - w) { found[0] = b; found[1] = end - w; found[2] = item_end - i; }
+      if (u0 < units_before + total) break;
+      units_before += total;
+      items_before += total_items;
+    }
   }
   __syncthreads();
   int b = __builtin_amdgcn_readfirstlane((int)found[0]);
-  long long seq_begin = found[1];
-  Split split{0, 0, 0, 0, 0, 0};
+  long long seq_begin = found[1], seq_item = found[2];
   Seq s = seq_of(a, b);
+  Split split{};
 
   for (long long u = u0; u < u1;) {
     while (u >= seq_begin + seq_units(a, s)) {               // on to the next sequence with rows
+      if (b + 1 >= a.c.n_seqs) return;                       // (units that do not add up: row_ptr or lens changed under the call)
       seq_begin += seq_units(a, s);
+      seq_item += (long long)s.tiles * a.c.n_kv_heads;
       s = seq_of(a, ++b);
     }
     const long long local = u - seq_begin;
@@ -412,11 +441,11 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
     int k0 = first * kUnit + wave * kStep;
     StepData<D> x;
     unsigned there = 0;
-    int page = -1;
+    int page = 0, after = 0;                                 // of the step at hand's successor, and of the one behind that
     if (k0 < end) {
       page = load_page(a.c, table, k0, end);
-      const int after = load_page(a.c, table, k0 + kUnit, end);
-      there = step_pages(a.c, page);
+      after = load_page(a.c, table, k0 + kUnit, end);
+      there = step_pages(a.c, page, k0, end);
       load_values<D>(x, a.c, head_piece, pb, page, k0);
       load_keys<D>(x, a.c, head_piece, pb, page, k0);
       page = after;
@@ -434,12 +463,13 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
       const unsigned now = there;
-      there = step_pages(a.c, page);
+      there = step_pages(a.c, page, k0 + kUnit, end);
+      after = load_page(a.c, table, k0 + 2 * kUnit, end);    // (first: loads complete in order)
       load_values<D>(x, a.c, head_piece, pb, page, k0 + kUnit);
       float s[16];
       score_step<D, TERMS>(s, x, ks, qf);
       load_keys<D>(x, a.c, head_piece, pb, page, k0 + kUnit);
-      page = load_page(a.c, table, k0 + 2 * kUnit, end);
+      page = after;
       softmax_step<D, TERMS>(st, s, vs, vp, now != 15 || k0 + kStep > all_see, k0, limit, now, a.scale_log2);
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
@@ -491,78 +521,93 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
         }
       } else {
         float* part = part_of<D>(ws, id, first == 0 ? 1 : 0);
-        store_out<E>(part + c * D + e0, out);
-        if (e0 == 0) { part[kCols * D + c] = m; part[kCols * D + kCols + c] = l; }
-        if (first == 0)
-          split = {id, block_of(seq_begin + (long long)item * s.units + s.units - 1, U, n) - id + 1, s.row0, cols, col0, hk * a.group};
+        if (c < cols) {
+          store_out<E>(part + c * D + e0, out);
+          if (e0 == 0) { part[kCols * D + c] = m; part[kCols * D + kCols + c] = l; }
+        }
       }
+    }
+    if (first == 0) {
+      split = Split{id, 0, s.row0, cols, col0, hk * a.group, {0, 0}};
+      if (last < s.units) split.parts = block_of(seq_begin + (long long)item * s.units + s.units - 1, U, n) - id + 1;
+      if (a.slots && tid == 0 && seq_item + item < a.slots) split_list(ws)[seq_item + item] = split;
     }
     __syncthreads();
     u += last - first;
   }
-  if (tid == 0) *reinterpret_cast<Split*>(ws + sizeof(Header) + (size_t)id * 32) = split;
+  if (!a.slots && tid == 0) split_list(ws)[id] = split;      // the last item it began: the one it may not have ended
 }
 
-// Adds up the parts of the item that block `blockIdx.x` of the first launch began and did not end, column blockIdx.y: 8 runs of parts
-// (thread / 32) of four channels each.
+// Adds up the parts of the split item listed at blockIdx.x, columns blockIdx.y, + gridDim.y, ...: runs of parts (thread / (D/4)) of four channels each,
+// in a fixed order.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(AttnArgs a, T* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws) {
   constexpr int W = D / 4, R = kThreads / W;                 // threads of a row of D channels; runs
-  const int i = blockIdx.x, c = blockIdx.y, tid = threadIdx.x;
-  if (i >= reinterpret_cast<const Header*>(ws)->blocks) return;
-  const Split s = *reinterpret_cast<const Split*>(ws + sizeof(Header) + (size_t)i * 32);
-  if (s.parts == 0 || c >= s.cols) return;
-  __shared__ float weight[kMaxGrid], red[kWaves];
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= reinterpret_cast<const Header*>(ws)->listed) return;
+  const Split s = split_list(ws)[blockIdx.x];
+  if (s.parts == 0) return;
+  __shared__ float weight[kMaxGrid], red[2 * kWaves];
   __shared__ float sums[R][D + 4];
   auto part = [&](int p) { return part_of<D>(ws, s.first + p, p == 0 ? 1 : 0); };
-  float m = -INFINITY;
-  for (int p = tid; p < s.parts; p += kThreads) {
-    const float x = part(p)[kCols * D + c];
-    weight[p] = x;
-    m = fmaxf(m, x);
+  for (int c = blockIdx.y; c < s.cols; c += gridDim.y) {
+    float m = -INFINITY, ms[kMaxGrid / kThreads], ls[kMaxGrid / kThreads];
+#pragma unroll
+    for (int i = 0; i < kMaxGrid / kThreads; ++i) {
+      const int p = tid + i * kThreads;
+      ms[i] = p < s.parts ? part(p)[kCols * D + c] : -INFINITY;
+      ls[i] = p < s.parts ? part(p)[kCols * D + kCols + c] : 0.f;
+      m = fmaxf(m, ms[i]);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if ((tid & 63) == 0) red[tid >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxGrid / kThreads; ++i) {
+      const int p = tid + i * kThreads;
+      const float f = __builtin_amdgcn_exp2f(ms[i] - ref);
+      if (p < s.parts) weight[p] = f;
+      l = __builtin_fmaf(ls[i], f, l);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+    if ((tid & 63) == 0) red[kWaves + (tid >> 6)] = l;
+    __syncthreads();
+    l = (red[kWaves] + red[kWaves + 1]) + (red[kWaves + 2] + red[kWaves + 3]);
+    const int run = tid / W, e = (tid % W) * 4;
+    floatx4v x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int p = run; p < s.parts; p += R) x += *reinterpret_cast<const floatx4v*>(part(p) + c * D + e) * weight[p];
+    *reinterpret_cast<floatx4v*>(&sums[run][e]) = x;
+    __syncthreads();
+    if (run == 0) {
+#pragma unroll
+      for (int r = 1; r < R; ++r) x += *reinterpret_cast<const floatx4v*>(&sums[r][e]);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      float out[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) out[k] = l == 0.f ? 0.f : x[k] * inv;
+      const int r = s.row0 + (s.col0 + c) / a.group, hd = s.head0 + (s.col0 + c) % a.group;
+      store_out<4>(o + ((size_t)r * a.Hq + hd) * D + e, out);
+      if (lse && e == 0) lse[(size_t)hd * a.c.n_rows + r] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+    __syncthreads();
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-  if ((tid & 63) == 0) red[tid >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float ref = m == -INFINITY ? 0.f : m;
-  __syncthreads();
-  float l = 0.f;
-  for (int p = tid; p < s.parts; p += kThreads) {
-    const float f = __builtin_amdgcn_exp2f(weight[p] - ref);
-    weight[p] = f;
-    l = __builtin_fmaf(part(p)[kCols * D + kCols + c], f, l);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
-  if ((tid & 63) == 0) red[tid >> 6] = l;
-  __syncthreads();
-  l = (red[0] + red[1]) + (red[2] + red[3]);
-  const int run = tid / W, e = (tid % W) * 4;
-  floatx4v x = {0.f, 0.f, 0.f, 0.f};
-  for (int p = run; p < s.parts; p += R) x += *reinterpret_cast<const floatx4v*>(part(p) + c * D + e) * weight[p];
-  *reinterpret_cast<floatx4v*>(&sums[run][e]) = x;
-  __syncthreads();
-  if (run != 0) return;
-#pragma unroll
-  for (int r = 1; r < R; ++r) x += *reinterpret_cast<const floatx4v*>(&sums[r][e]);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  float out[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) out[k] = l == 0.f ? 0.f : x[k] * inv;
-  const int r = s.row0 + (s.col0 + c) / a.group, hd = s.head0 + (s.col0 + c) % a.group;
-  store_out<4>(o + ((size_t)r * a.Hq + hd) * D + e, out);
-  if (lse && e == 0) lse[(size_t)hd * a.c.n_rows + r] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Items there can be: tiles of 16 columns of each sequence, at most one more than its columns fill.
+long long most_items(const slimattn_cache_params& p, int n_q_heads) {
+  return ((long long)p.n_rows * (n_q_heads / p.n_kv_heads) / kCols + p.n_seqs) * p.n_kv_heads;
+}
 // Blocks of the first launch: as many as there can be units, up to what is resident at once.
 int grid_blocks(const slimattn_cache_params& p, int n_q_heads) {
   const int resident = 256 * (p.dtype == SLIMATTN_BF16 ? (p.head_dim == 128 ? kBlocksPerCu<128, 1> : kBlocksPerCu<64, 1>)
                                                        : (p.head_dim == 128 ? kBlocksPerCu<128, 3> : kBlocksPerCu<64, 3>));
-  const long long cols = (long long)p.n_rows * (n_q_heads / p.n_kv_heads);
-  const long long items = (cols / kCols + p.n_seqs) * p.n_kv_heads;
-  const long long units = ((long long)p.max_pages * p.page_size + kUnit - 1) / kUnit;
+  const long long items = most_items(p, n_q_heads), units = ((long long)p.max_pages * p.page_size + kUnit - 1) / kUnit;
   const long long most = items > resident ? resident : items * units;
   return (int)(most < resident ? most : resident);
 }
@@ -573,16 +618,21 @@ CacheView cache_view(const slimattn_cache_params& p, const int32_t* row_ptr, con
 
 size_t cache_attn_bytes(const slimattn_cache_params& p, int n_q_heads) {
   const size_t part = (size_t)(kCols * p.head_dim + 2 * kCols) * sizeof(float);
-  return sizeof(Header) + (size_t)kMaxGrid * 32 + (size_t)grid_blocks(p, n_q_heads) * 2 * part;
+  return sizeof(Header) + kMaxGrid * sizeof(Split) + (size_t)grid_blocks(p, n_q_heads) * 2 * part;
 }
 
 int launch_cache_attn(const slimattn_cache_params& p, int n_q_heads, float scale, const void* q, const int32_t* row_ptr, const int32_t* lens,
                       const int32_t* table, const void* cache, void* o, float* lse, void* ws, void* stream) {
-  AttnArgs a{cache_view(p, row_ptr, lens, table), n_q_heads / p.n_kv_heads, n_q_heads, 0.f, 1.f};
+  AttnArgs a{cache_view(p, row_ptr, lens, table), n_q_heads / p.n_kv_heads, n_q_heads, 0.f, 1.f, 0};
   const float f = scale * 1.4426950408889634f, size = f < 0.f ? -f : f;
   a.q_sign = f < 0.f ? -1.f : f > 0.f ? 1.f : 0.f;
   a.scale_log2 = size > 0x1p-126f ? size : 0x1p-126f;        // masked scores are -inf times it
   const int blocks = grid_blocks(p, n_q_heads);
+  // Few items are listed by their number, so that few blocks look for work in the second launch, and each of theirs may have hundreds of
+  // parts: a block per column.  Many are listed by the block that began them, with few parts each: four columns.
+  const long long items = most_items(p, n_q_heads);
+  a.slots = items < blocks ? (int)items : 0;
+  const dim3 join(a.slots ? a.slots : blocks, a.slots && a.slots <= 64 ? kCols : 4);
   auto run = [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value, TERMS = sizeof(T) == 4 ? 3 : 1;
@@ -590,7 +640,7 @@ int launch_cache_attn(const slimattn_cache_params& p, int n_q_heads, float scale
                        (T*)o, lse, (char*)ws);
     const int e = (int)hipGetLastError();
     if (e != 0 || blocks < 2) return e;                      // one block holds every item whole
-    hipLaunchKernelGGL((cache_attn_join_kernel<T, D>), dim3((unsigned)blocks, kCols), dim3(kThreads), 0, (hipStream_t)stream, a, (T*)o, lse, (char*)ws);
+    hipLaunchKernelGGL((cache_attn_join_kernel<T, D>), join, dim3(kThreads), 0, (hipStream_t)stream, a, (T*)o, lse, (char*)ws);
     return (int)hipGetLastError();
   };
   if (p.dtype == SLIMATTN_F32) return p.head_dim == 128 ? run(float{}, IC<128>{}) : run(float{}, IC<64>{});

@@ -285,18 +285,27 @@ __global__ __launch_bounds__(kThreads) void rope_bwd_kernel(RopeArgs a, const T*
   }
 }
 
-// dq_weight[c], dk_weight[c] = sum over blocks of partial[block][..][c]: 16 columns per block, 16 strided sums of each, added in a fixed order.
-__global__ __launch_bounds__(kThreads) void rope_weight_kernel(const float* __restrict__ partial, int n_blocks, int D, float* dqw, float* dkw) {
-  __shared__ float sums[16][17];
+// dq_weight[c], dk_weight[c] = sum over blocks of partial[block][..][c]: 16 columns per block, 64 strided sums of each, added in a fixed order.
+// The partial sums lie behind another launch's stores, a microsecond away: 16 of a thread's at most 16 loads are on their way at once (with 16
+// sums of 64 loads one after the other 21 us, so about 3).
+constexpr int kWeightRuns = 64;
+__global__ __launch_bounds__(16 * kWeightRuns) void rope_weight_kernel(const float* __restrict__ partial, int n_blocks, int D, float* dqw, float* dkw) {
+  __shared__ float sums[kWeightRuns][17];
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
-  float s = 0.f;
-  for (int b = r; b < n_blocks; b += 16) s += partial[(size_t)b * 2 * D + col];
+  float x[kBwdBlocks / kWeightRuns], s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kBwdBlocks / kWeightRuns; ++i) {
+    const int b = r + i * kWeightRuns;
+    x[i] = b < n_blocks ? partial[(size_t)b * 2 * D + col] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < kBwdBlocks / kWeightRuns; ++i) s += x[i];
   sums[r][c] = s;
   __syncthreads();
   if (r != 0) return;
   s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += sums[i][c];
+  for (int i = 0; i < kWeightRuns; ++i) s += sums[i][c];
   float* out = col < D ? dqw : dkw;
   if (out) out[col < D ? col : col - D] = s;
 }
@@ -371,7 +380,7 @@ int launch_bwd(const slimattn_rope_params& p, const void* q, const void* k, cons
       if (e != 0) return e;
     }
     if (!weights) return 0;
-    hipLaunchKernelGGL(rope_weight_kernel, dim3(2 * D / 16), dim3(kThreads), 0, (hipStream_t)stream, (const float*)ws, blocks, D, dqw, dkw);
+    hipLaunchKernelGGL(rope_weight_kernel, dim3(2 * D / 16), dim3(16 * kWeightRuns), 0, (hipStream_t)stream, (const float*)ws, blocks, D, dqw, dkw);
     return (int)hipGetLastError();
   });
 }
