@@ -18,47 +18,42 @@
 // through the wave's own LDS, where the 4-bit transpose read turns rows of V into the operand's columns.
 #include <hip/hip_runtime.h>
 
-#include "cache.h"
+#include "cache_attn.h"
 
 namespace slimattn {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
 constexpr int kCols = 16;            // query columns of a tile
 constexpr int kStep = 64;            // keys of a wave's step
 constexpr int kUnit = kWaves * kStep;
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kMaxGrid = 1024;       // at most four blocks per compute unit
 
-struct AttnArgs {
-  CacheView c;
-  int group, Hq;                     // query heads per KV head; of all
-  float scale_log2;                  // > 0
-  float q_sign;                      // scale < 0 turns q around; 0 makes it zero
-  int slots;                         // split items are listed by number if there are at most this many items, 0: by the block that began them
+// What a sequence of few columns adds to the row of units: every tile of every head its length in units.
+struct NarrowRow {
+  int row0, rows, len, tiles, units, heads;
+  __device__ __forceinline__ NarrowRow(const AttnArgs& a, int b) {
+    seq_rows(a, b, row0, rows, len);
+    heads = a.c.n_kv_heads;
+    const long long cols = (long long)rows * a.group;
+    tiles = cols > a.narrow_cols ? 0 : (int)((cols + kCols - 1) / kCols);
+    units = max(1, (len + kUnit - 1) / kUnit);               // rows that see nothing are items too: their outputs are written
+  }
+  __device__ __forceinline__ long long units_of_all() const { return (long long)tiles * units * heads; }
+  __device__ __forceinline__ long long items() const { return (long long)tiles * heads; }
+  __device__ __forceinline__ static int blocks(const AttnArgs&, int most, long long units, long long) { return (int)min((long long)most, units); }
+  static constexpr bool kNeedsItems = false;
 };
-
-// An item that blocks share, written by the one that holds its start for the launch that adds its parts up (parts = 0: not shared).
-struct Split { int first, parts, row0, cols, col0, head0, pad[2]; };
-struct Header { int listed, pad[7]; };   // entries that were written
-__device__ __forceinline__ Split* split_list(char* ws) { return reinterpret_cast<Split*>(ws + sizeof(Header)); }
 
 template <int D> constexpr int kPartFloats = kCols * D + 2 * kCols;   // [col][D], max [col], sum [col]
 
 template <int D>
 __device__ __forceinline__ float* part_of(char* ws, int block, int slot) {
-  return reinterpret_cast<float*>(ws + sizeof(Header) + kMaxGrid * sizeof(Split)) + ((size_t)block * 2 + slot) * kPartFloats<D>;
+  return reinterpret_cast<float*>(ws + 2 * kListBytes) + ((size_t)block * 2 + slot) * kPartFloats<D>;
 }
 
-typedef float floatx4v __attribute__((ext_vector_type(4)));
 typedef int int2v __attribute__((ext_vector_type(2)));
 template <int D> struct Piece;                    // what a lane loads of D/2 bytes x 16 keys, or of the scales
 template <> struct Piece<128> { typedef uint4 type; typedef uint2 scale; };
 template <> struct Piece<64> { typedef uint2 type; typedef unsigned scale; };
-
-__device__ __forceinline__ unsigned word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-__device__ __forceinline__ unsigned word(const uint2& v, int i) { return i == 0 ? v.x : v.y; }
-__device__ __forceinline__ unsigned word(unsigned v, int) { return v; }
 
 __device__ __forceinline__ floatx4v mfma16(bf16x8 a, bf16x8 b, floatx4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -270,52 +265,6 @@ __device__ __forceinline__ void softmax_step(State<D>& st, float (&s)[16], float
   });
 }
 
-// What a sequence contributes to the row of units: its rows, tiles, units per tile.
-struct Seq { int row0, rows, len, tiles, units; };
-
-__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int b) {
-  Seq s;
-  s.row0 = b;
-  s.rows = 1;
-  if (a.c.row_ptr) {
-    s.row0 = min(max(a.c.row_ptr[b], 0), a.c.n_rows);
-    s.rows = min(max(a.c.row_ptr[b + 1], s.row0), a.c.n_rows) - s.row0;
-  }
-  s.len = seq_len(a.c, b);
-  s.tiles = (int)(((long long)s.rows * a.group + kCols - 1) / kCols);
-  s.units = max(1, (s.len + kUnit - 1) / kUnit);             // rows that see nothing are items too: their outputs are written
-  return s;
-}
-__device__ __forceinline__ long long seq_units(const AttnArgs& a, const Seq& s) { return (long long)s.tiles * s.units * a.c.n_kv_heads; }
-
-__device__ __forceinline__ long long wave_scan(long long x) {   // inclusive
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long y = __shfl_up(x, d);
-    if ((int)(threadIdx.x & 63) >= d) x += y;
-  }
-  return x;
-}
-
-// Inclusive scan over the block; `total` gets the sum.
-__device__ __forceinline__ long long block_scan(long long x, long long* lds, long long& total) {
-  x = wave_scan(x);
-  const int wave = threadIdx.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) lds[wave] = x;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) x += lds[w];
-    total += lds[w];
-  }
-  return x;
-}
-
-// The block that holds unit x of U, when block i of n holds units [U i / n, U (i + 1) / n).
-__device__ __forceinline__ int block_of(long long x, long long U, int n) { return (int)(((x + 1) * n - 1) / U); }
-
 template <class T> __device__ __forceinline__ void load_q(const T* p, float sign, float (&x)[8]);
 template <> __device__ __forceinline__ void load_q<bf16>(const bf16* p, float sign, float (&x)[8]) {
   const uint4 w = *reinterpret_cast<const uint4*>(p);
@@ -325,17 +274,6 @@ template <> __device__ __forceinline__ void load_q<bf16>(const bf16* p, float si
 template <> __device__ __forceinline__ void load_q<float>(const float* p, float sign, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = sign * p[i];
-}
-
-template <int N>
-__device__ __forceinline__ void store_out(bf16* p, const float (&x)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) *reinterpret_cast<bf16x4*>(p + i) = bf16x4{(bf16)x[i], (bf16)x[i + 1], (bf16)x[i + 2], (bf16)x[i + 3]};
-}
-template <int N>
-__device__ __forceinline__ void store_out(float* p, const float (&x)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) *reinterpret_cast<floatx4v*>(p + i) = floatx4v{x[i], x[i + 1], x[i + 2], x[i + 3]};
 }
 
 template <class T, int D, int TERMS>
@@ -349,55 +287,23 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
   // neighbouring blocks of the row of units on one XCD: tiles of one head read the same keys
   const int id = N % 8 == 0 ? (int)(blockIdx.x % 8) * (N / 8) + blockIdx.x / 8 : blockIdx.x;
 
-  // the row of units: its length, then the sequence in which this block's first unit lies.  Up to 256 sequences are one look at the lengths.
-  const bool one_look = a.c.n_seqs <= kThreads;
-  long long U = 0, items = 0, mine = 0, my_items = 0;
-  for (int b0 = 0; b0 < a.c.n_seqs; b0 += kThreads) {
-    const int b = b0 + tid;
-    if (b < a.c.n_seqs) {
-      const Seq s = seq_of(a, b);
-      mine += seq_units(a, s);
-      my_items += (long long)s.tiles * a.c.n_kv_heads;
-    }
-  }
-  const long long units_to = block_scan(mine, scan, U), items_to = a.slots ? block_scan(my_items, scan, items) : 0;
-  const int n = (int)min((long long)N, U);                   // blocks with work: no unit, no block
-  if (blockIdx.x == 0 && tid == 0) reinterpret_cast<Header*>(ws)->listed = a.slots ? (int)min((long long)a.slots, items) : n;
-  if (id >= n) return;
-  const long long u0 = U * id / n, u1 = U * (id + 1) / n;
-  if (one_look) {
-    if (u0 < units_to && u0 >= units_to - mine) { found[0] = tid; found[1] = units_to - mine; found[2] = items_to - my_items; }
-  } else {
-    long long units_before = 0, items_before = 0;
-    for (int b0 = 0;; b0 += kThreads) {                      // ends: u0 < U
-      const int b = b0 + tid;
-      long long w = 0, i = 0, total, total_items = 0;
-      if (b < a.c.n_seqs) {
-        const Seq s = seq_of(a, b);
-        w = seq_units(a, s);
-        i = (long long)s.tiles * a.c.n_kv_heads;
-      }
-      const long long end = units_before + block_scan(w, scan, total);
-      const long long item_end = a.slots ? items_before + block_scan(i, scan, total_items) : 0;
-      if (u0 < end && u0 >= end - w) { found[0] = b; found[1] = end - w; found[2] = item_end - i; }
-      if (u0 < units_before + total) break;
-      units_before += total;
-      items_before += total_items;
-    }
-  }
-  __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane((int)found[0]);
-  long long seq_begin = found[1], seq_item = found[2];
-  Seq s = seq_of(a, b);
+  Place place;
+  if (!find_place<NarrowRow>(a, N, id, scan, found, split_header(ws), place)) return;
+  const int n = place.blocks;
+  const long long U = place.total, u0 = place.begin, u1 = place.end;
+  int b = place.seq;
+  long long seq_begin = place.seq_begin, seq_item = place.seq_item;
+  NarrowRow s(a, b);
   Split split{};
 
   for (long long u = u0; u < u1;) {
-    while (u >= seq_begin + seq_units(a, s)) {               // on to the next sequence with rows
-      if (b + 1 >= a.c.n_seqs) return;                       // (units that do not add up: row_ptr or lens changed under the call)
-      seq_begin += seq_units(a, s);
-      seq_item += (long long)s.tiles * a.c.n_kv_heads;
-      s = seq_of(a, ++b);
+    while (u >= seq_begin + s.units_of_all()) {               // on to the next sequence with rows
+      if (b + 1 >= a.c.n_seqs) { u = u1; break; }            // (units that do not add up: row_ptr or lens changed under the call)
+      seq_begin += s.units_of_all();
+      seq_item += s.items();
+      s = NarrowRow(a, ++b);
     }
+    if (u >= u1) break;
     const long long local = u - seq_begin;
     const int item = __builtin_amdgcn_readfirstlane((int)(local / s.units)), first = __builtin_amdgcn_readfirstlane((int)(local % s.units));
     const int last = (int)min((long long)s.units, first + (u1 - u));
@@ -530,12 +436,12 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
     if (first == 0) {
       split = Split{id, 0, s.row0, cols, col0, hk * a.group, {0, 0}};
       if (last < s.units) split.parts = block_of(seq_begin + (long long)item * s.units + s.units - 1, U, n) - id + 1;
-      if (a.slots && tid == 0 && seq_item + item < a.slots) split_list(ws)[seq_item + item] = split;
+      if (a.slots && tid == 0 && seq_item + item < a.slots) split_list(split_header(ws))[seq_item + item] = split;
     }
     __syncthreads();
     u += last - first;
   }
-  if (!a.slots && tid == 0) split_list(ws)[id] = split;      // the last item it began: the one it may not have ended
+  if (!a.slots && tid == 0) split_list(split_header(ws))[id] = split;      // the last item it began: the one it may not have ended
 }
 
 // Adds up the parts of the split item listed at blockIdx.x, columns blockIdx.y, + gridDim.y, ...: runs of parts (thread / (D/4)) of four channels each,
@@ -544,8 +450,8 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(AttnArgs a, T* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws) {
   constexpr int W = D / 4, R = kThreads / W;                 // threads of a row of D channels; runs
   const int tid = threadIdx.x;
-  if ((int)blockIdx.x >= reinterpret_cast<const Header*>(ws)->listed) return;
-  const Split s = split_list(ws)[blockIdx.x];
+  if ((int)blockIdx.x >= split_header(ws)->listed) return;
+  const Split s = split_list(split_header(ws))[blockIdx.x];
   if (s.parts == 0) return;
   __shared__ float weight[kMaxGrid], red[2 * kWaves];
   __shared__ float sums[R][D + 4];
@@ -615,18 +521,42 @@ int grid_blocks(const slimattn_cache_params& p, int n_q_heads) {
 }  // namespace
 
 CacheView cache_view(const slimattn_cache_params& p, const int32_t* row_ptr, const int32_t* lens, const int32_t* table);
+size_t cache_attn_wide_bytes(const slimattn_cache_params& p, int n_q_heads);
+int launch_cache_attn_wide(const slimattn_cache_params& p, int n_q_heads, AttnArgs a, const void* q, const void* cache, void* o, float* lse, void* ws,
+                           size_t parts_at, void* stream);
+
+namespace {
+
+// Which kernel takes a sequence goes by its number of query columns, which the device knows (row_ptr).  A tile of 128 columns takes the wide kernel
+// about as long as NARROW_MEASURED tiles of 16 the narrow one.
+constexpr long long kNarrowCols = 48;
+bool may_be_wide(const slimattn_cache_params& p, int n_q_heads, bool ragged) {
+  return p.dtype == SLIMATTN_BF16 && (ragged ? p.n_rows : 1ll) * (n_q_heads / p.n_kv_heads) > kNarrowCols;
+}
+// One sequence has all the rows there are: it is taken to be wide, and the narrow kernel has nothing to do.
+bool all_wide(const slimattn_cache_params& p, int n_q_heads, bool ragged) { return may_be_wide(p, n_q_heads, ragged) && (!ragged || p.n_seqs == 1); }
+
+size_t narrow_bytes(const slimattn_cache_params& p, int n_q_heads) {
+  return (size_t)grid_blocks(p, n_q_heads) * 2 * (kCols * p.head_dim + 2 * kCols) * sizeof(float);
+}
+
+}  // namespace
 
 size_t cache_attn_bytes(const slimattn_cache_params& p, int n_q_heads) {
-  const size_t part = (size_t)(kCols * p.head_dim + 2 * kCols) * sizeof(float);
-  return sizeof(Header) + kMaxGrid * sizeof(Split) + (size_t)grid_blocks(p, n_q_heads) * 2 * part;
+  return 2 * kListBytes + narrow_bytes(p, n_q_heads) + (may_be_wide(p, n_q_heads, true) || may_be_wide(p, n_q_heads, false) ? cache_attn_wide_bytes(p, n_q_heads) : 0);
 }
 
 int launch_cache_attn(const slimattn_cache_params& p, int n_q_heads, float scale, const void* q, const int32_t* row_ptr, const int32_t* lens,
                       const int32_t* table, const void* cache, void* o, float* lse, void* ws, void* stream) {
-  AttnArgs a{cache_view(p, row_ptr, lens, table), n_q_heads / p.n_kv_heads, n_q_heads, 0.f, 1.f, 0};
+  const bool wide = may_be_wide(p, n_q_heads, row_ptr != nullptr), narrow = !all_wide(p, n_q_heads, row_ptr != nullptr);
+  AttnArgs a{cache_view(p, row_ptr, lens, table), n_q_heads / p.n_kv_heads, n_q_heads, 0.f, 1.f, !wide ? INT64_MAX : narrow ? kNarrowCols : 0, 0};
   const float f = scale * 1.4426950408889634f, size = f < 0.f ? -f : f;
   a.q_sign = f < 0.f ? -1.f : f > 0.f ? 1.f : 0.f;
   a.scale_log2 = size > 0x1p-126f ? size : 0x1p-126f;        // masked scores are -inf times it
+  if (wide) {
+    const int e = launch_cache_attn_wide(p, n_q_heads, a, q, cache, o, lse, ws, 2 * kListBytes + narrow_bytes(p, n_q_heads), stream);
+    if (e != 0 || !narrow) return e;
+  }
   const int blocks = grid_blocks(p, n_q_heads);
   // Few items are listed by their number, so that few blocks look for work in the second launch, and each of theirs may have hundreds of
   // parts: a block per column.  Many are listed by the block that began them, with few parts each: four columns.

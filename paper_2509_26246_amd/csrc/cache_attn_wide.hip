@@ -1,0 +1,484 @@
+// Attention over the 4-bit cache for sequences with many query columns (rows x heads of the group): slices of prompts, bf16.
+//
+// The narrow kernel (cache_attn.hip) unpacks the cache once for 16 columns and scales scores and probabilities; with many columns that is most of its
+// time.  Here a block of four waves takes 128 columns, and unpacks each tile of 64 keys once for all of them into LDS, scales applied: every value of
+// the cache is exactly a bf16 number, so S^T = K q and O^T += V^T P^T on 32x32x16 products lose nothing against the codes.  Each wave keeps 32
+// columns (a lane holds one column's scores, so sums and maxima need one lane exchange), tiles are double-buffered, and the next tile's codes are loaded a
+// tile ahead and unpacked between the two products of this one.
+//
+// Bound by the vector unit: per wave and tile 32 products of 32 cycles against 32 exponentials of 16, and about 130 instructions to unpack a quarter
+// of the next tile; two blocks share a compute unit, so one's products run beside the other's softmax.
+//
+// Work.  A tile's columns see the keys up to their last row, so the tiles of one prompt differ in length: a tile weighs (keys before the rows + a fixed
+// part) * group + its last column's number, which adds up to a closed form over tiles; weights are divided evenly among the blocks, cuts fall on
+// whole tiles of keys.  Parts leave O, maximum and sum of 128 columns in the workspace (67 KB at head dim 128): blocks are only used as far as each has
+// the work of 256 keys, or an item of its own.
+#include <hip/hip_runtime.h>
+
+#include "cache_attn.h"
+
+namespace slimattn {
+namespace {
+
+constexpr int kCols = 128;           // query columns of a block, 32 per wave
+constexpr int kKeys = 64;            // keys of a tile
+constexpr int kFixedKeys = 192;      // what an item costs beside its keys (its queries, its output), in keys
+constexpr int kLeastKeys = 256;      // work that is worth a block and its parts
+constexpr float kLazy = 8.f;         // the reference moves where a score exceeds it by more than this (log2): probabilities stay below 256
+
+template <int D> constexpr int kPartFloats = kCols * D + 2 * kCols;
+template <int D>
+__device__ __forceinline__ float* part_of(char* parts, int block, int slot) { return reinterpret_cast<float*>(parts) + ((size_t)block * 2 + slot) * kPartFloats<D>; }
+
+// What a sequence of many columns adds to the row of work: tile t of a head weighs weight(t), tiles 0 .. t-1 before(t).
+struct WideRow {
+  int row0, rows, len, tiles, heads, group;
+  long long a;
+  __device__ __forceinline__ WideRow(const AttnArgs& x, int b) {
+    seq_rows(x, b, row0, rows, len);
+    heads = x.c.n_kv_heads;
+    group = x.group;
+    const long long cols = (long long)rows * group;
+    tiles = cols > x.narrow_cols ? (int)((cols + kCols - 1) / kCols) : 0;
+    a = (long long)(max(len - rows, 0) + kFixedKeys) * group;
+  }
+  __device__ __forceinline__ long long weight(long long t) const { return a + kCols * (t + 1); }
+  __device__ __forceinline__ long long before(long long t) const { return t * a + kCols * (t * (t + 1) / 2); }
+  __device__ __forceinline__ long long units_of_all() const { return before(tiles) * heads; }
+  __device__ __forceinline__ long long items() const { return (long long)tiles * heads; }
+  // The tile in which unit y of a head lies: the root of before(t) = y, corrected for its rounding.
+  __device__ __forceinline__ int tile_of(long long y) const {
+    const double p = (double)a + 0.5 * kCols;
+    long long t = (long long)((__builtin_sqrt(p * p + 2.0 * kCols * (double)y) - p) / kCols);
+    t = min(max(t, 0ll), (long long)tiles - 1);
+    while (t > 0 && before(t) > y) --t;
+    while (t + 1 < tiles && before(t + 1) <= y) ++t;
+    return (int)t;
+  }
+  // Keys of the cut at `w` of an item's weight.
+  __device__ __forceinline__ int keys_at(long long w) const { return (int)max(w / group - kFixedKeys, 0ll) & ~(kKeys - 1); }
+  __device__ __forceinline__ static int blocks(const AttnArgs& x, int most, long long units, long long items) {
+    return (int)min((long long)most, max(items, units / ((long long)kLeastKeys * x.group)));
+  }
+  static constexpr bool kNeedsItems = true;
+};
+
+// This thread's piece of a tile on its way: row tid / 4 (a wave's rows are one chunk of 16 keys), piece tid % 4 of its codes, and the scales.
+template <int D>
+struct Stage {
+  static constexpr int G = D / 32;
+  unsigned k[G], v[G], ks[G / 2], vs;
+  int page;                          // of the wave's chunk, -1 without one (uniform)
+};
+
+template <int D>
+__device__ __forceinline__ void load_stage(Stage<D>& x, const CacheView& c, const char* head, unsigned pb, int entry, int k0, int end) {
+  constexpr int G = D / 32;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), key = k0 + kCacheChunk * wave;
+  entry = __builtin_amdgcn_readfirstlane(entry);
+  x.page = key < end && (unsigned)entry < (unsigned)c.n_pages ? entry : -1;
+  const int t = (key & ((1 << c.page_shift) - 1)) + (tid >> 2 & 15), j = tid & 3;
+  const char* base = head + (size_t)(unsigned)max(x.page, 0) * pb;
+  const unsigned* kp = reinterpret_cast<const unsigned*>(base + key_codes<D>(t)) + j * G;
+  const unsigned* vp = reinterpret_cast<const unsigned*>(base + value_codes<D>(c, t)) + j * G;
+  const unsigned* sp = reinterpret_cast<const unsigned*>(base + scales<D>(c, 0, t));
+  if constexpr (G == 4) {
+    const uint4 a = *reinterpret_cast<const uint4*>(kp), b = *reinterpret_cast<const uint4*>(vp);
+    const uint2 s = *reinterpret_cast<const uint2*>(sp);
+    x.k[0] = a.x; x.k[1] = a.y; x.k[2] = a.z; x.k[3] = a.w;
+    x.v[0] = b.x; x.v[1] = b.y; x.v[2] = b.z; x.v[3] = b.w;
+    x.ks[0] = s.x; x.ks[1] = s.y;
+  } else {
+    const uint2 a = *reinterpret_cast<const uint2*>(kp), b = *reinterpret_cast<const uint2*>(vp);
+    x.k[0] = a.x; x.k[1] = a.y;
+    x.v[0] = b.x; x.v[1] = b.y;
+    x.ks[0] = *sp;
+  }
+  x.vs = *reinterpret_cast<const unsigned short*>(base + scales<D>(c, 1, t) + 2 * (j * G / 4));
+}
+// The table's entry for the wave's chunk of a tile, kept in a vector register until it is used: a scalar one would be waited for here.
+__device__ __forceinline__ int load_entry(const CacheView& c, const int32_t* table, int k0, int end) {
+  int at = min(k0 + kCacheChunk * (int)(threadIdx.x >> 6), end - 1) >> c.page_shift;
+  asm volatile("" : "+v"(at));
+  return table[at];
+}
+
+// Four codes (half a word, `hi`) times their scale.
+__device__ __forceinline__ bf16x4 unpack4(unsigned w, bool hi, float s) {
+  typedef float float2v __attribute__((ext_vector_type(2)));
+  const float2v a = hi ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0);
+  const float2v b = hi ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
+  return __builtin_convertvector((floatx4){a.x * s, a.y * s, b.x * s, b.y * s}, bf16x4);
+}
+
+// LDS: [buffer][K tile, V tile], then per buffer what the tile's four chunks are (bit 0: there is a page, bit 1: a value scale that columns must
+// not see unless they see its key) and which groups of a key's values those are.
+template <int D> constexpr int kTileBytes = kKeys * D * 2;
+template <int D> constexpr int kInfoAt = 4 * kTileBytes<D>;
+constexpr int kInfoBytes = 16 + kKeys * 4;
+template <int D> constexpr int kLdsBytes = kInfoAt<D> + 2 * kInfoBytes;
+
+// The swizzle of a tile (lds_off16) is an exclusive or on address bits 4 to 7, and tiles begin at multiples of 256 bytes: what changes with a fragment's
+// column is an exclusive or with a constant, so one address register serves them all.
+__device__ __forceinline__ lds_cptr flip_bits(lds_cptr p, int bits) { return (lds_cptr)(unsigned)((unsigned)(uintptr_t)p ^ bits); }
+
+// Where this thread's pieces of a tile go in a buffer: its first K word (channels 8 j ..; word g: address bits g << 6 flipped) and its first V word
+// (channels 8 j G ..; word i: i << 4).
+template <int D>
+__device__ __forceinline__ int unpack_keys_at() { return lds_off16<D>(threadIdx.x >> 2, threadIdx.x & 3); }
+template <int D>
+__device__ __forceinline__ int unpack_values_at() { return kTileBytes<D> + lds_off16<D>(threadIdx.x >> 2, (threadIdx.x & 3) * (D / 32)); }
+// The value scale of this thread's piece.  end: behind the last key that some column of the block sees: values from there on may be anything and
+// become zeros.  bad: a scale that is not finite, which columns must not notice unless they see its key (zeros here, too: note_stage, then
+// the softmax).
+template <int D>
+__device__ __forceinline__ float value_scale(const Stage<D>& x, int k0, int end, bool& bad) {
+  const float s = lo_bf16(x.vs);
+  const bool seen = x.page >= 0 && k0 + (int)(threadIdx.x >> 2) < end, finite = s - s == 0.f;
+  bad = seen && !finite;
+  return seen && finite ? s : 0.f;
+}
+// Half of word n (key words, then value words) of the piece: n = slot / 2.  `part` takes the first half to the second.
+template <int D>
+__device__ __forceinline__ void unpack_slot(const Stage<D>& x, lds_cptr keys, lds_cptr values, int slot, float vs, bf16x4& part) {
+  constexpr int G = D / 32;
+  const int n = slot >> 1;
+  const float s = n >= G ? vs : n & 1 ? hi_bf16(x.ks[n / 2]) : lo_bf16(x.ks[n / 2]);
+  unsigned w = n >= G ? x.v[n - G] : x.k[n];
+  asm volatile("" : "+v"(w));                                // (here, not ahead of the products)
+  const bf16x4 y = unpack4(w, slot & 1, s);
+  if (slot & 1)
+    *(LDS_PTR(bf16x8))(n >= G ? flip_bits(values, (n - G) << 4) : flip_bits(keys, n << 6)) = __builtin_shufflevector(part, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  else part = y;
+}
+template <int D>
+__device__ __forceinline__ bool unpack_stage(const Stage<D>& x, lds_cptr keys, lds_cptr values, int k0, int end) {
+  bool bad;
+  const float vs = value_scale<D>(x, k0, end, bad);
+  bf16x4 part;
+#pragma unroll
+  for (int slot = 0; slot < D / 8; ++slot) unpack_slot<D>(x, keys, values, slot, vs, part);
+  return bad;
+}
+// What the wave's chunk of that tile is.
+template <int D>
+__device__ __forceinline__ void note_stage(const Stage<D>& x, LDS_PTR(char) lds, int buf, bool bad) {
+  constexpr int G = D / 32;
+  const int tid = threadIdx.x, row = tid >> 2, j = tid & 3;
+  LDS_PTR(int) info = (LDS_PTR(int))(lds + kInfoAt<D> + buf * kInfoBytes);
+  const bool any = __any(bad);
+  info[tid >> 6] = (x.page >= 0 ? 1 : 0) | (any ? 2 : 0);    // (the wave's lanes write the same)
+  if (any) {
+    int groups = bad ? 1 << (j * G / 4) : 0;
+    groups |= __shfl_xor(groups, 1);
+    groups |= __shfl_xor(groups, 2);
+    if (j == 0) info[4 + row] = groups;
+  }
+}
+
+// Fragment f, issued before at most N later LDS operations, has landed.
+template <int N>
+__device__ __forceinline__ void wait_frag(bf16x8& f) { asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(f) : "n"(N)); }
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a, const bf16* __restrict__ q, const char* __restrict__ cache, bf16* __restrict__ o,
+                                                                      float* __restrict__ lse, char* __restrict__ ws, size_t parts_at) {
+  constexpr int NKS = D / 16, NDB = D / 32, G = D / 32;
+  __shared__ __attribute__((aligned(1024))) char smem[kLdsBytes<D>];
+  __shared__ long long scan[kWaves], found[3];
+  LDS_PTR(char) lds = (LDS_PTR(char))smem;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+  const int N = gridDim.x;
+  const int id = N % 8 == 0 ? (int)(blockIdx.x % 8) * (N / 8) + blockIdx.x / 8 : blockIdx.x;   // neighbours in the row of work on one XCD
+  Header* header = split_header(ws + kListBytes);
+  Place place;
+  if (!find_place<WideRow>(a, N, id, scan, found, header, place)) return;
+  int b = place.seq;
+  long long seq_begin = place.seq_begin, seq_item = place.seq_item;
+  WideRow s(a, b);
+  Split split{};
+
+  for (long long u = place.begin; u < place.end;) {
+    while (u >= seq_begin + s.units_of_all()) {              // on to the next sequence with tiles
+      if (b + 1 >= a.c.n_seqs) { u = place.end; break; }     // (units that do not add up: row_ptr or lens changed under the call)
+      seq_begin += s.units_of_all();
+      seq_item += s.items();
+      s = WideRow(a, ++b);
+    }
+    if (u >= place.end) break;
+    const long long per_head = s.before(s.tiles), local = u - seq_begin, head_begin = local / per_head * per_head;
+    const int hk = __builtin_amdgcn_readfirstlane((int)(local / per_head)), t = __builtin_amdgcn_readfirstlane(s.tile_of(local - head_begin));
+    const long long item_begin = seq_begin + head_begin + s.before(t), from = u - item_begin, to = min(s.weight(t), from + (place.end - u));
+    const bool first = from == 0, last = to == s.weight(t);
+    const long long col0 = (long long)t * kCols;             // columns of a sequence: rows * group may pass 32 bits
+    const int cols = (int)min((long long)s.rows * a.group - col0, (long long)kCols);
+    const int base = s.len - s.rows, row_first = (int)(col0 / a.group), in_row = (int)(col0 % a.group);
+    const int mine = wave * 32 + l32, row = row_first + (in_row + mine) / a.group, head = hk * a.group + (in_row + mine) % a.group;
+    const bool real = mine < cols;
+    const int limit = real ? base + row : -1;
+    const int visible = base + row_first + (in_row + cols - 1) / a.group + 1;
+    const int wave_all = base + row_first + (in_row + wave * 32) / a.group + 1;                 // keys that all of the wave's columns see
+    const int wave_end = wave * 32 < cols ? base + row_first + (in_row + min(wave * 32 + 31, cols - 1)) / a.group + 1 : 0;
+    const int k_begin = first ? 0 : __builtin_amdgcn_readfirstlane(s.keys_at(from));
+    const int k_end = __builtin_amdgcn_readfirstlane(last ? visible : min(s.keys_at(to), visible));
+
+    bf16x8 qf[NKS];
+    {
+      const bf16* qp = q + ((size_t)(s.row0 + (real ? row : 0)) * a.Hq + (real ? head : 0)) * D + 8 * half;
+      const unsigned flip = a.q_sign < 0.f ? 0x80008000u : 0u, keep = real && a.q_sign != 0.f ? 0xffffffffu : 0u;
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {
+        uint4 w = *reinterpret_cast<const uint4*>(qp + 16 * ks);
+        w.x = (w.x ^ flip) & keep; w.y = (w.y ^ flip) & keep; w.z = (w.z ^ flip) & keep; w.w = (w.w ^ flip) & keep;
+        qf[ks] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+    floatx16 oacc[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    const int32_t* table = a.c.table + (size_t)b * a.c.max_pages;
+    const char* piece = cache + hk * head_bytes<D>(a.c);
+    const unsigned pb = (unsigned)page_bytes<D>(a.c);
+    if (k_begin < k_end) {
+      // two tiles on their way beside the one at hand: a tile takes about as long as a load from memory
+      Stage<D> xa, xb;
+      const int e0 = load_entry(a.c, table, k_begin, k_end), e1 = load_entry(a.c, table, k_begin + kKeys, k_end);
+      int entry = load_entry(a.c, table, k_begin + 2 * kKeys, k_end);
+      load_stage<D>(xa, a.c, piece, pb, e0, k_begin, k_end);
+      load_stage<D>(xb, a.c, piece, pb, e1, k_begin + kKeys, k_end);
+      __syncthreads();                                       // the buffers are free
+      note_stage<D>(xa, lds, 0, unpack_stage<D>(xa, lds + unpack_keys_at<D>(), lds + unpack_values_at<D>(), k_begin, visible));
+      const int e2 = entry;
+      entry = load_entry(a.c, table, k_begin + 3 * kKeys, k_end);
+      load_stage<D>(xa, a.c, piece, pb, e2, k_begin + 2 * kKeys, k_end);
+      __syncthreads();
+      lds_cptr pk = lds_row_ptr<D>(lds, l32, 8 * half), pv0, pv1;   // this buffer's fragments; the other's unpacked pieces
+      lds_tr_ptrs<D>(lds + kTileBytes<D>, 0, lane, pv0, pv1);
+      lds_cptr uk = keep(lds + 2 * kTileBytes<D> + unpack_keys_at<D>()), uv = keep(lds + 2 * kTileBytes<D> + unpack_values_at<D>());
+      // Tile k0, in buffer BUF; x holds the next tile and takes the one three tiles on.  (The last tiles load and unpack again what nobody reads: no
+      // branch between the products.)
+      auto tile = [&](auto buf_, Stage<D>& x, const int k0) {
+        constexpr int buf = decltype(buf_)::value;
+        if (k0 < wave_end) {
+          // S^T = K q; a product's share of the unpacking follows it
+          constexpr int NF = 2 * NKS, kAhead = 4;
+          floatx16 sacc[2];
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sacc[kb][r] = 0.f;
+          bf16x8 f[NF];
+          bf16x4 part;
+          bool bad;
+          const float vs = value_scale<D>(x, k0 + kKeys, visible, bad);
+          static_for<0, kAhead>([&](auto i_) {
+            constexpr int i = decltype(i_)::value;
+            r1_issue<(i & 1) * 64 * D>(flip_bits(pk, (i >> 1) << 5), f[i]);
+          });
+          static_for<0, NF>([&](auto i_) {
+            constexpr int i = decltype(i_)::value;
+            wait_frag<(NF - 1 - i < kAhead - 1 ? NF - 1 - i : kAhead - 1)>(f[i]);
+            sacc[i & 1] = mfma32(f[i], qf[i >> 1], sacc[i & 1]);
+            if constexpr (i + kAhead < NF) r1_issue<(i & 1) * 64 * D>(flip_bits(pk, ((i + kAhead) >> 1) << 5), f[i + kAhead]);
+            unpack_slot<D>(x, uk, uv, i, vs, part);
+            __builtin_amdgcn_sched_barrier(0);
+          });
+          LDS_PTR(const int) info = (LDS_PTR(const int))(lds + kInfoAt<D> + buf * kInfoBytes);
+          const int i0 = info[0], i1 = info[1], i2 = info[2], i3 = info[3];
+          note_stage<D>(x, lds, buf ^ 1, bad);
+          const int all = __builtin_amdgcn_readfirstlane(i0 & i1 & i2 & i3), some = __builtin_amdgcn_readfirstlane(i0 | i1 | i2 | i3);
+          if (!(all & 1) || k0 + kKeys > wave_all) {         // key 32 kb + 8 (r / 4) + 4 half + r % 4 of the tile
+            const int rel = limit - k0 - 4 * half;
+            const int there = (i0 & 1) | (i1 & 1) << 1 | (i2 & 1) << 2 | (i3 & 1) << 3;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (32 * kb + 8 * (r >> 2) + (r & 3) > rel || !(there >> (2 * kb + (r >> 3)) & 1)) sacc[kb][r] = -INFINITY;
+          }
+          float mx = sacc[0][0];
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[kb][r]);
+          mx = fmaxf(mx, xor32(mx)) * a.scale_log2;
+          if (__any(mx > m + kLazy)) {
+            const float to_m = fmaxf(m, mx), alpha = to_m == m ? 1.f : __builtin_amdgcn_exp2f(m - to_m);
+            m = to_m;
+            l *= alpha;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+          }
+          const float ref = m == -INFINITY ? 0.f : m;        // nothing seen yet: every score is -inf
+          bf16x8 pf[4];
+          float sum[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            sum[j] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = 8 * (j & 1) + i;
+              sacc[j >> 1][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[j >> 1][r], a.scale_log2, -ref));
+              sum[j] += sacc[j >> 1][r];
+            }
+            pf[j] = pack8(sacc[j >> 1], 8 * (j & 1));
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          // O^T += V^T P^T: one batch of four V^T fragments (the four 16-key steps) per block of 32 channels
+          Tr4 tb[NDB];
+          constexpr int kRows = 32 * D;
+          tr4_issue<0, kRows, 2 * kRows, 3 * kRows>(pv0, pv1, tb[0]);
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) {
+            if (db + 1 < NDB) tr4_issue_wait<0, kRows, 2 * kRows, 3 * kRows>(flip_bits(pv0, (db + 1) << 6), flip_bits(pv1, (db + 1) << 6), tb[db + 1], tb[db]);
+            else tr4_wait(tb[db]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) oacc[db] = mfma32(tr4_frag(tb[db], j), pf[j], oacc[db]);
+          }
+          if (some & 2) {                                    // a value scale that is not finite: NaN where its key is seen
+            int hit = 0;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int chunk = 2 * kb + (r >> 3), ci = chunk == 0 ? i0 : chunk == 1 ? i1 : chunk == 2 ? i2 : i3;
+                const int groups = info[4 + 32 * kb + 8 * (r >> 2) + 4 * half + (r & 3)];
+                hit |= (ci & 2) != 0 & sacc[kb][r] != 0.f ? groups : 0;
+              }
+            hit |= __shfl_xor(hit, 32);
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) {
+              const float poison = hit >> db & 1 ? __builtin_nanf("") : 0.f;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) oacc[db][r] += poison;
+            }
+          }
+        } else {                                             // nothing that this wave's columns see: only fetch
+          note_stage<D>(x, lds, buf ^ 1, unpack_stage<D>(x, uk, uv, k0 + kKeys, visible));
+        }
+        const int entry_now = entry;                         // (one place for both ways: a copy of what is loaded would wait for it)
+        entry = load_entry(a.c, table, k0 + 4 * kKeys, k_end);   // (first: loads complete in order)
+        load_stage<D>(x, a.c, piece, pb, entry_now, k0 + 3 * kKeys, k_end);
+        constexpr int to_other = buf ? -2 * kTileBytes<D> : 2 * kTileBytes<D>;
+        pk += to_other; pv0 += to_other; pv1 += to_other;
+        uk -= to_other; uv -= to_other;
+        // this tile's reads and the next one's writes are done (loads on their way may stay so)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      };
+      for (int k0 = k_begin; k0 < k_end; k0 += 2 * kKeys) {
+        tile(IC<0>{}, xb, k0);
+        if (k0 + kKeys < k_end) tile(IC<1>{}, xa, k0 + kKeys);
+      }
+    }
+
+    l += xor32(l);
+    if (first && last) {
+      if (real) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bf16* op = o + ((size_t)(s.row0 + row) * a.Hq + head) * D + 4 * half;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const float x[4] = {l == 0.f ? 0.f : oacc[db][r] * inv, l == 0.f ? 0.f : oacc[db][r + 1] * inv, l == 0.f ? 0.f : oacc[db][r + 2] * inv,
+                                l == 0.f ? 0.f : oacc[db][r + 3] * inv};
+            store_out<4>(op + 32 * db + 2 * r, x);
+          }
+        if (lse && half == 0) lse[(size_t)head * a.c.n_rows + s.row0 + row] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+      }
+    } else {
+      float* part = part_of<D>(ws + parts_at, id, first ? 1 : 0);
+      if (real) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<floatx4v*>(part + mine * D + 32 * db + 2 * r + 4 * half) = floatx4v{oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]};
+        if (half == 0) { part[kCols * D + mine] = m; part[kCols * D + kCols + mine] = l; }
+      }
+    }
+    if (first) {
+      const long long item_end = item_begin + s.weight(t);
+      split = Split{id, 0, s.row0 + row_first, cols, in_row, hk * a.group, {0, 0}};
+      if (!last) split.parts = block_of(item_end - 1, place.total, place.blocks) - id + 1;
+      const long long number = seq_item + (long long)hk * s.tiles + t;
+      if (a.slots && tid == 0 && number < a.slots) split_list(header)[number] = split;
+    }
+    u += to - from;
+  }
+  if (!a.slots && tid == 0) split_list(header)[id] = split;
+}
+
+// Adds up the parts of the split item listed at blockIdx.x, in order: a thread has four channels of one column.
+template <int D>
+__global__ __launch_bounds__(kThreads) void cache_attn_wide_join_kernel(AttnArgs a, bf16* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws, size_t parts_at) {
+  constexpr int W = D / 4;
+  Header* header = split_header(ws + kListBytes);
+  if ((int)blockIdx.x >= header->listed) return;
+  const Split s = split_list(header)[blockIdx.x];
+  const int c = blockIdx.y * (kThreads / W) + threadIdx.x / W, e = threadIdx.x % W * 4;
+  if (s.parts == 0 || c >= s.cols) return;
+  auto part = [&](int p) { return part_of<D>(ws + parts_at, s.first + p, p == 0 ? 1 : 0); };
+  float m = -INFINITY;
+#pragma unroll 8
+  for (int p = 0; p < s.parts; ++p) m = fmaxf(m, part(p)[kCols * D + c]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  floatx4v x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int p = 0; p < s.parts; ++p) {
+    const float* y = part(p);
+    const float f = __builtin_amdgcn_exp2f(y[kCols * D + c] - ref);
+    l = __builtin_fmaf(y[kCols * D + kCols + c], f, l);
+    x += *reinterpret_cast<const floatx4v*>(y + c * D + e) * f;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int r = s.row0 + (s.col0 + c) / a.group, hd = s.head0 + (s.col0 + c) % a.group;
+  const float out[4] = {l == 0.f ? 0.f : x[0] * inv, l == 0.f ? 0.f : x[1] * inv, l == 0.f ? 0.f : x[2] * inv, l == 0.f ? 0.f : x[3] * inv};
+  store_out<4>(o + ((size_t)r * a.Hq + hd) * D + e, out);
+  if (lse && e == 0) lse[(size_t)hd * a.c.n_rows + r] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+long long most_items(const slimattn_cache_params& p, int n_q_heads) {
+  return ((long long)p.n_rows * (n_q_heads / p.n_kv_heads) / kCols + p.n_seqs) * p.n_kv_heads;
+}
+// Two blocks per compute unit, fewer where there cannot be work for them.
+int grid_blocks(const slimattn_cache_params& p, int n_q_heads) {
+  const long long items = most_items(p, n_q_heads), keys = (long long)p.max_pages * p.page_size + kFixedKeys + 1;
+  const long long most = items > 512 ? 512 : items * (keys / kLeastKeys + 1);
+  return (int)(most < 512 ? most : 512);
+}
+
+}  // namespace
+
+size_t cache_attn_wide_bytes(const slimattn_cache_params& p, int n_q_heads) {
+  return (size_t)grid_blocks(p, n_q_heads) * 2 * (kCols * p.head_dim + 2 * kCols) * sizeof(float);
+}
+
+int launch_cache_attn_wide(const slimattn_cache_params& p, int n_q_heads, AttnArgs a, const void* q, const void* cache, void* o, float* lse, void* ws,
+                           size_t parts_at, void* stream) {
+  const int blocks = grid_blocks(p, n_q_heads);
+  const long long items = most_items(p, n_q_heads);
+  a.slots = items < blocks ? (int)items : 0;
+  auto run = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    hipLaunchKernelGGL((cache_attn_wide_kernel<D>), dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, a, (const bf16*)q, (const char*)cache,
+                       (bf16*)o, lse, (char*)ws, parts_at);
+    const int e = (int)hipGetLastError();
+    if (e != 0 || blocks < 2) return e;
+    hipLaunchKernelGGL((cache_attn_wide_join_kernel<D>), dim3(a.slots ? a.slots : blocks, kCols * (D / 4) / kThreads), dim3(kThreads), 0, (hipStream_t)stream, a,
+                       (bf16*)o, lse, (char*)ws, parts_at);
+    return (int)hipGetLastError();
+  };
+  return p.head_dim == 128 ? run(IC<128>{}) : run(IC<64>{});
+}
+
+}  // namespace slimattn

@@ -230,6 +230,26 @@ def test_a_prompt_slice(dtype):
     _attend([333, 210], [200, 210], 4, 4, 64, dtype, 16)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(8, 1), (6, 2), (5, 5), (20, 1), (64, 1)])
+def test_many_query_columns(d, hq, hkv):
+    # tiles of 128 columns that end inside a row's heads, keys that end inside a tile, prompts with and without keys before them
+    _attend([200, 64, 65, 0, 77], [90, 64, 65, 30, 100], hq, hkv, d, "bf16", 16)
+    _attend([1200], [100], hq, hkv, d, "bf16", 256)
+
+
+def test_many_query_columns_over_long_keys():
+    _attend([9000], [37], 8, 1, 128, "bf16", 64)           # few items, their keys divided among blocks
+    _attend([5000, 33, 2500], [40, 33, 1], 8, 2, 64, "bf16", 32, qf=8.0)
+    _attend([70, 3000], [1, 60], 64, 1, 64, "bf16", 64)    # 64 columns of one row
+
+
+def test_prompts_beside_single_tokens():
+    lens = [130, 500, 64, 1, 300, 9]
+    _attend(lens, [130, 1, 20, 1, 2, 0], 8, 2, 128, "bf16", 16)
+    _attend([300] * 5, [1] * 5, 64, 1, 128, "bf16", 16, ptr=False)
+
+
 def test_many_sequences():
     r = np.random.default_rng(3)
     lens = [int(x) for x in r.integers(0, 90, 700)]        # more than the blocks' scan takes at once
@@ -248,24 +268,32 @@ def test_sharp_scores_and_no_lse(dtype):
     _attend([600, 90], [1, 4], 4, 2, 128, dtype, 16, qf=30.0, want_lse=False)
 
 
-def test_infinities_behind_a_rows_position_are_not_seen():
-    # the last token's keys and values are NaN: earlier rows must not notice, rows that see it must
-    hq, hkv, d, dt, n = 2, 1, 64, torch.bfloat16, 100
+@pytest.mark.parametrize("dtype,hq,rows", [("bf16", 2, 3), ("f32", 2, 3), ("bf16", 8, 30), ("bf16", 16, 70)])
+def test_infinities_behind_a_rows_position_are_not_seen(dtype, hq, rows):
+    # the keys or values of the second last token are NaN: earlier rows must not notice, the two that see it must
+    hkv, d, dt, n = 1, 64, DT[dtype], 100
     for spoil in ("k", "v"):
-        c = _cache([n], hkv, d, dt, 16, max_rows=3, hq=hq)
+        c = _cache([n], hkv, d, dt, 16, max_rows=rows, hq=hq)
         k, v = _values((n, hkv, d), 1, dt), _values((n, hkv, d), 2, dt)
-        (k if spoil == "k" else v)[-1] = float("nan")
+        (k if spoil == "k" else v)[-2, :, :32] = float("nan")
         c.write(k.cuda(), v.cuda(), _ptr([n]))
-        q = _values((3, hq, d), 3, dt, False)
-        o = torch.empty(3, hq, d, dtype=dt, device="cuda")
-        lse = torch.empty(hq, 3, device="cuda")
-        c.attend(q.cuda(), o, lse, 0.125, _ptr([3]))
-        _check_attend(o[:2], lse[:, :2], q[:2], R.held(k)[:-1], R.held(v)[:-1], [n - 1], [2], 2, 0.125, dt)
-        assert torch.isnan(o[2]).all()
+        q = _values((rows, hq, d), 3, dt, False)
+        o = torch.empty(rows, hq, d, dtype=dt, device="cuda")
+        lse = torch.empty(hq, rows, device="cuda")
+        c.attend(q.cuda(), o, lse, 0.125, _ptr([rows]))
+        _check_attend(o[:-2], lse[:, :-2].contiguous(), q[:-2], R.held(k)[:-2], R.held(v)[:-2], [n - 2], [rows - 2], hq, 0.125, dt)
+        assert torch.isnan(o[-2:] if spoil == "k" else o[-2:, :, :32]).all()
+        if spoil == "v":                                   # the other scale group's channels are not spoilt
+            clean = R.held(v)
+            clean[-2, :, :32] = 0
+            want, _, size = R.attend(q[-2:], R.held(k), clean, hq, 0.125, n - 2)
+            err = (o[-2:, :, 32:].double().cpu() - want[..., 32:]).abs()
+            assert (err <= 2.0 ** -6 * (size[..., 32:] + want[..., 32:].abs())).all()
 
 
-def test_pages_that_are_not_there_are_not_seen():
-    hq, hkv, d, dt, n = 4, 2, 128, torch.bfloat16, 200
+@pytest.mark.parametrize("hq", [4, 128])
+def test_pages_that_are_not_there_are_not_seen(hq):
+    hkv, d, dt, n = 2, 128, torch.bfloat16, 200
     c = _cache([n, n], hkv, d, dt, 32, max_rows=2, hq=hq, extra=0)
     k, v = _values((2 * n, hkv, d), 1, dt), _values((2 * n, hkv, d), 2, dt)
     c.write(k.cuda(), v.cuda(), _ptr([n, n]))
@@ -277,7 +305,7 @@ def test_pages_that_are_not_there_are_not_seen():
     keep1 = [n + j for j in range(n) if j // 32 not in (0, 6)]
     kh, vh = R.held(k), R.held(v)
     for b, keep in enumerate((keep0, keep1)):
-        _check_attend(o[b:b + 1], lse[:, b:b + 1], q[b:b + 1], kh[keep], vh[keep], [len(keep)], [1], 2, 0.1, dt)
+        _check_attend(o[b:b + 1], lse[:, b:b + 1], q[b:b + 1], kh[keep], vh[keep], [len(keep)], [1], hq // 2, 0.1, dt)
     c.page_table.fill_(-1)
     c.attend(q.cuda(), o, lse, 0.1)
     assert (o == 0).all() and torch.isneginf(lse).all()
