@@ -24,7 +24,9 @@ constexpr int kCols = 128;           // query columns of a block, 32 per wave
 constexpr int kKeys = 64;            // keys of a tile
 constexpr int kFixedKeys = 192;      // what an item costs beside its keys (its queries, its output), in keys
 constexpr int kLeastKeys = 256;      // work that is worth a block and its parts
-constexpr float kLazy = 8.f;         // the reference moves where a score exceeds it by more than this (log2): probabilities stay below 256
+constexpr float kLazySum = 4096.f;   // the reference moves where a lane's sum of 16 probabilities exceeds this (or is not a number)
+
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 
 template <int D> constexpr int kPartFloats = kCols * D + 2 * kCols;
 template <int D>
@@ -63,22 +65,32 @@ struct WideRow {
   static constexpr bool kNeedsItems = true;
 };
 
+// The thread's number, as something to compute with here and now: offsets derived from it would otherwise be kept in registers through the walk, which
+// has none to spare.
+__device__ __forceinline__ int thread_number() {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
 // This thread's piece of a tile on its way: row tid / 4 (a wave's rows are one chunk of 16 keys), piece tid % 4 of its codes, and the scales.
 template <int D>
 struct Stage {
   static constexpr int G = D / 32;
   unsigned k[G], v[G], ks[G / 2], vs;
-  int page;                          // of the wave's chunk, -1 without one (uniform)
+  int there;                         // bit c: the tile's chunk c is in a page (uniform)
 };
 
+// entry: lanes l hold the table's entry for chunk l % 4.  Chunks without a page take page 0 and are masked.
 template <int D>
 __device__ __forceinline__ void load_stage(Stage<D>& x, const CacheView& c, const char* head, unsigned pb, int entry, int k0, int end) {
   constexpr int G = D / 32;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), key = k0 + kCacheChunk * wave;
-  entry = __builtin_amdgcn_readfirstlane(entry);
-  x.page = key < end && (unsigned)entry < (unsigned)c.n_pages ? entry : -1;
+  const int tid = thread_number(), wave = __builtin_amdgcn_readfirstlane(tid >> 6), key = k0 + kCacheChunk * wave;
+  const bool good = (unsigned)entry < (unsigned)c.n_pages && k0 + kCacheChunk * (tid & 3) < end;
+  x.there = (int)(__ballot(good) & 15);
+  const int page = x.there >> wave & 1 ? __builtin_amdgcn_readlane(entry, wave) : 0;
   const int t = (key & ((1 << c.page_shift) - 1)) + (tid >> 2 & 15), j = tid & 3;
-  const char* base = head + (size_t)(unsigned)max(x.page, 0) * pb;
+  const char* base = head + (size_t)(unsigned)page * pb;
   const unsigned* kp = reinterpret_cast<const unsigned*>(base + key_codes<D>(t)) + j * G;
   const unsigned* vp = reinterpret_cast<const unsigned*>(base + value_codes<D>(c, t)) + j * G;
   const unsigned* sp = reinterpret_cast<const unsigned*>(base + scales<D>(c, 0, t));
@@ -96,11 +108,9 @@ __device__ __forceinline__ void load_stage(Stage<D>& x, const CacheView& c, cons
   }
   x.vs = *reinterpret_cast<const unsigned short*>(base + scales<D>(c, 1, t) + 2 * (j * G / 4));
 }
-// The table's entry for the wave's chunk of a tile, kept in a vector register until it is used: a scalar one would be waited for here.
+// The table's entry for chunk lane % 4 of a tile.
 __device__ __forceinline__ int load_entry(const CacheView& c, const int32_t* table, int k0, int end) {
-  int at = min(k0 + kCacheChunk * (int)(threadIdx.x >> 6), end - 1) >> c.page_shift;
-  asm volatile("" : "+v"(at));
-  return table[at];
+  return table[min(k0 + kCacheChunk * (thread_number() & 3), end - 1) >> c.page_shift];
 }
 
 // Four codes (half a word, `hi`) times their scale.
@@ -111,12 +121,12 @@ __device__ __forceinline__ bf16x4 unpack4(unsigned w, bool hi, float s) {
   return __builtin_convertvector((floatx4){a.x * s, a.y * s, b.x * s, b.y * s}, bf16x4);
 }
 
-// LDS: [buffer][K tile, V tile], then per buffer what the tile's four chunks are (bit 0: there is a page, bit 1: a value scale that columns must
-// not see unless they see its key) and which groups of a key's values those are.
+// LDS: [buffer][K tile, V tile], then per buffer and wave whether its chunk of the tile has scales that are not finite, and which of a key's groups
+// those are (bits 0 .. G-1 values, 8 keys).
 template <int D> constexpr int kTileBytes = kKeys * D * 2;
-template <int D> constexpr int kInfoAt = 4 * kTileBytes<D>;
-constexpr int kInfoBytes = 16 + kKeys * 4;
-template <int D> constexpr int kLdsBytes = kInfoAt<D> + 2 * kInfoBytes;
+template <int D> constexpr int kBadAt = 4 * kTileBytes<D>;
+constexpr int kBadBytes = 16 + kKeys * 4;
+template <int D> constexpr int kLdsBytes = kBadAt<D> + 2 * kBadBytes;
 
 // The swizzle of a tile (lds_off16) is an exclusive or on address bits 4 to 7, and tiles begin at multiples of 256 bytes: what changes with a fragment's
 // column is an exclusive or with a constant, so one address register serves them all.
@@ -128,62 +138,80 @@ template <int D>
 __device__ __forceinline__ int unpack_keys_at() { return lds_off16<D>(threadIdx.x >> 2, threadIdx.x & 3); }
 template <int D>
 __device__ __forceinline__ int unpack_values_at() { return kTileBytes<D> + lds_off16<D>(threadIdx.x >> 2, (threadIdx.x & 3) * (D / 32)); }
-// The value scale of this thread's piece.  end: behind the last key that some column of the block sees: values from there on may be anything and
-// become zeros.  bad: a scale that is not finite, which columns must not notice unless they see its key (zeros here, too: note_stage, then
-// the softmax).
+// The scales of this thread's piece, those of its keys per group, then its values'.  Chunks without a page and keys from `end` on (behind the last that
+// some column of the block sees) may hold anything: their scales become zeros, and the softmax masks them.  So do scales that are not
+// finite, which only columns that see their key may notice: bad (note_bad; the softmax makes NaN of them for those columns).
 template <int D>
-__device__ __forceinline__ float value_scale(const Stage<D>& x, int k0, int end, bool& bad) {
-  const float s = lo_bf16(x.vs);
-  const bool seen = x.page >= 0 && k0 + (int)(threadIdx.x >> 2) < end, finite = s - s == 0.f;
-  bad = seen && !finite;
-  return seen && finite ? s : 0.f;
+struct Scales { float k[D / 32], v; int bad; };
+template <int D>
+__device__ __forceinline__ Scales<D> piece_scales(const Stage<D>& x, int k0, int end) {
+  constexpr int G = D / 32;
+  const int tid = thread_number(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool seen = (x.there >> wave & 1) && k0 + (tid >> 2) < end;
+  Scales<D> s;
+  s.bad = 0;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const float f = g & 1 ? hi_bf16(x.ks[g / 2]) : lo_bf16(x.ks[g / 2]);
+    const bool finite = f - f == 0.f;
+    s.k[g] = seen && finite ? f : 0.f;
+    s.bad |= seen && !finite ? 256 : 0;
+  }
+  const float f = lo_bf16(x.vs);
+  const bool finite = f - f == 0.f;
+  s.v = seen && finite ? f : 0.f;
+  s.bad |= seen && !finite ? 1 << ((tid & 3) * G / 4) : 0;
+  return s;
 }
 // Half of word n (key words, then value words) of the piece: n = slot / 2.  `part` takes the first half to the second.
 template <int D>
-__device__ __forceinline__ void unpack_slot(const Stage<D>& x, lds_cptr keys, lds_cptr values, int slot, float vs, bf16x4& part) {
+__device__ __forceinline__ void unpack_slot(const Stage<D>& x, lds_cptr keys, lds_cptr values, int slot, const Scales<D>& s, bf16x4& part) {
   constexpr int G = D / 32;
   const int n = slot >> 1;
-  const float s = n >= G ? vs : n & 1 ? hi_bf16(x.ks[n / 2]) : lo_bf16(x.ks[n / 2]);
   unsigned w = n >= G ? x.v[n - G] : x.k[n];
   asm volatile("" : "+v"(w));                                // (here, not ahead of the products)
-  const bf16x4 y = unpack4(w, slot & 1, s);
+  const bf16x4 y = unpack4(w, slot & 1, n >= G ? s.v : s.k[n]);
   if (slot & 1)
     *(LDS_PTR(bf16x8))(n >= G ? flip_bits(values, (n - G) << 4) : flip_bits(keys, n << 6)) = __builtin_shufflevector(part, y, 0, 1, 2, 3, 4, 5, 6, 7);
   else part = y;
 }
+// What is not finite in the wave's chunk.
 template <int D>
-__device__ __forceinline__ bool unpack_stage(const Stage<D>& x, lds_cptr keys, lds_cptr values, int k0, int end) {
-  bool bad;
-  const float vs = value_scale<D>(x, k0, end, bad);
+__device__ __forceinline__ void note_bad(LDS_PTR(char) lds, int buf, int bad) {
+  const int tid = thread_number();
+  LDS_PTR(int) info = (LDS_PTR(int))(lds + kBadAt<D> + buf * kBadBytes);
+  const bool any = __any(bad != 0);
+  info[tid >> 6] = any;                                      // (the wave's lanes write the same)
+  if (any) {
+    bad |= __shfl_xor(bad, 1);
+    bad |= __shfl_xor(bad, 2);
+    if ((tid & 3) == 0) info[4 + (tid >> 2)] = bad;
+  }
+}
+template <int D>
+__device__ __forceinline__ void unpack_stage(const Stage<D>& x, LDS_PTR(char) lds, int buf, lds_cptr keys, lds_cptr values, int k0, int end) {
+  const Scales<D> s = piece_scales<D>(x, k0, end);
   bf16x4 part;
 #pragma unroll
-  for (int slot = 0; slot < D / 8; ++slot) unpack_slot<D>(x, keys, values, slot, vs, part);
-  return bad;
-}
-// What the wave's chunk of that tile is.
-template <int D>
-__device__ __forceinline__ void note_stage(const Stage<D>& x, LDS_PTR(char) lds, int buf, bool bad) {
-  constexpr int G = D / 32;
-  const int tid = threadIdx.x, row = tid >> 2, j = tid & 3;
-  LDS_PTR(int) info = (LDS_PTR(int))(lds + kInfoAt<D> + buf * kInfoBytes);
-  const bool any = __any(bad);
-  info[tid >> 6] = (x.page >= 0 ? 1 : 0) | (any ? 2 : 0);    // (the wave's lanes write the same)
-  if (any) {
-    int groups = bad ? 1 << (j * G / 4) : 0;
-    groups |= __shfl_xor(groups, 1);
-    groups |= __shfl_xor(groups, 2);
-    if (j == 0) info[4 + row] = groups;
-  }
+  for (int slot = 0; slot < D / 8; ++slot) unpack_slot<D>(x, keys, values, slot, s, part);
+  note_bad<D>(lds, buf, s.bad);
 }
 
 // Fragment f, issued before at most N later LDS operations, has landed.
 template <int N>
 __device__ __forceinline__ void wait_frag(bf16x8& f) { asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(f) : "n"(N)); }
+template <int N>
+__device__ __forceinline__ void wait_frag(short4v& a, short4v& b) { asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "n"(N)); }
+
+__device__ __forceinline__ bf16x8 join_frag(short4v a, short4v b) {
+  typedef __attribute__((__vector_size__(8 * sizeof(short)))) short short8v;
+  return __builtin_bit_cast(bf16x8, (short8v)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
 
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a, const bf16* __restrict__ q, const char* __restrict__ cache, bf16* __restrict__ o,
                                                                       float* __restrict__ lse, char* __restrict__ ws, size_t parts_at) {
-  constexpr int NKS = D / 16, NDB = D / 32, G = D / 32;
+  constexpr int NKS = D / 16, NDB = D / 32;
   __shared__ __attribute__((aligned(1024))) char smem[kLdsBytes<D>];
   __shared__ long long scan[kWaves], found[3];
   LDS_PTR(char) lds = (LDS_PTR(char))smem;
@@ -238,75 +266,91 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m = real ? -INFINITY : 0.f, l = 0.f;               // the reference (log2 units), the sum against it
 
     const int32_t* table = a.c.table + (size_t)b * a.c.max_pages;
     const char* piece = cache + hk * head_bytes<D>(a.c);
     const unsigned pb = (unsigned)page_bytes<D>(a.c);
     if (k_begin < k_end) {
-      // two tiles on their way beside the one at hand: a tile takes about as long as a load from memory
-      Stage<D> xa, xb;
+      Stage<D> x;                                            // the next tile, on its way
       const int e0 = load_entry(a.c, table, k_begin, k_end), e1 = load_entry(a.c, table, k_begin + kKeys, k_end);
       int entry = load_entry(a.c, table, k_begin + 2 * kKeys, k_end);
-      load_stage<D>(xa, a.c, piece, pb, e0, k_begin, k_end);
-      load_stage<D>(xb, a.c, piece, pb, e1, k_begin + kKeys, k_end);
+      load_stage<D>(x, a.c, piece, pb, e0, k_begin, k_end);
       __syncthreads();                                       // the buffers are free
-      note_stage<D>(xa, lds, 0, unpack_stage<D>(xa, lds + unpack_keys_at<D>(), lds + unpack_values_at<D>(), k_begin, visible));
-      const int e2 = entry;
-      entry = load_entry(a.c, table, k_begin + 3 * kKeys, k_end);
-      load_stage<D>(xa, a.c, piece, pb, e2, k_begin + 2 * kKeys, k_end);
+      unpack_stage<D>(x, lds, 0, lds + unpack_keys_at<D>(), lds + unpack_values_at<D>(), k_begin, visible);
+      int there = x.there, buf = 0;
+      load_stage<D>(x, a.c, piece, pb, e1, k_begin + kKeys, k_end);
       __syncthreads();
       lds_cptr pk = lds_row_ptr<D>(lds, l32, 8 * half), pv0, pv1;   // this buffer's fragments; the other's unpacked pieces
       lds_tr_ptrs<D>(lds + kTileBytes<D>, 0, lane, pv0, pv1);
       lds_cptr uk = keep(lds + 2 * kTileBytes<D> + unpack_keys_at<D>()), uv = keep(lds + 2 * kTileBytes<D> + unpack_values_at<D>());
-      // Tile k0, in buffer BUF; x holds the next tile and takes the one three tiles on.  (The last tiles load and unpack again what nobody reads: no
-      // branch between the products.)
-      auto tile = [&](auto buf_, Stage<D>& x, const int k0) {
-        constexpr int buf = decltype(buf_)::value;
-        if (k0 < wave_end) {
-          // S^T = K q; a product's share of the unpacking follows it
-          constexpr int NF = 2 * NKS, kAhead = 4;
-          floatx16 sacc[2];
+
+      // The products of tile k0, and between them the other work: x, the next tile, is unpacked beside the first half's scores and the
+      // second half's O^T products; a half's probabilities are formed beside the products that follow its scores.  A half is 32 keys.
+      // Fragments are read kAhead products ahead.  
+      auto products = [&](const int k0) {
+        constexpr int NF = 2 * NKS, NV = 4 * NDB, kAhead = 4;
+        const int limit_here = limit - (thread_number() >> 3 & 4);
+        const bool masked = there != 15 || k0 + kKeys > wave_all;
+        auto mask = [&](floatx16& s, int kb) {               // key 32 kb + 8 (r / 4) + 4 half + r % 4 of the tile
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+          for (int r = 0; r < 16; ++r)
+            if (32 * kb + 8 * (r >> 2) + (r & 3) > limit_here - k0 || !(there >> (2 * kb + (r >> 3)) & 1)) s[r] = -INFINITY;
+        };
+        floatx16 sacc[2];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sacc[kb][r] = 0.f;
-          bf16x8 f[NF];
-          bf16x4 part;
-          bool bad;
-          const float vs = value_scale<D>(x, k0 + kKeys, visible, bad);
-          static_for<0, kAhead>([&](auto i_) {
-            constexpr int i = decltype(i_)::value;
-            r1_issue<(i & 1) * 64 * D>(flip_bits(pk, (i >> 1) << 5), f[i]);
-          });
-          static_for<0, NF>([&](auto i_) {
-            constexpr int i = decltype(i_)::value;
-            wait_frag<(NF - 1 - i < kAhead - 1 ? NF - 1 - i : kAhead - 1)>(f[i]);
-            sacc[i & 1] = mfma32(f[i], qf[i >> 1], sacc[i & 1]);
-            if constexpr (i + kAhead < NF) r1_issue<(i & 1) * 64 * D>(flip_bits(pk, ((i + kAhead) >> 1) << 5), f[i + kAhead]);
-            unpack_slot<D>(x, uk, uv, i, vs, part);
-            __builtin_amdgcn_sched_barrier(0);
-          });
-          LDS_PTR(const int) info = (LDS_PTR(const int))(lds + kInfoAt<D> + buf * kInfoBytes);
-          const int i0 = info[0], i1 = info[1], i2 = info[2], i3 = info[3];
-          note_stage<D>(x, lds, buf ^ 1, bad);
-          const int all = __builtin_amdgcn_readfirstlane(i0 & i1 & i2 & i3), some = __builtin_amdgcn_readfirstlane(i0 | i1 | i2 | i3);
-          if (!(all & 1) || k0 + kKeys > wave_all) {         // key 32 kb + 8 (r / 4) + 4 half + r % 4 of the tile
-            const int rel = limit - k0 - 4 * half;
-            const int there = (i0 & 1) | (i1 & 1) << 1 | (i2 & 1) << 2 | (i3 & 1) << 3;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                if (32 * kb + 8 * (r >> 2) + (r & 3) > rel || !(there >> (2 * kb + (r >> 3)) & 1)) sacc[kb][r] = -INFINITY;
+        for (int r = 0; r < 16; ++r) sacc[0][r] = sacc[1][r] = 0.f;
+        bf16x8 kf[NF];
+        short4v vf[NV][2];
+        // (the second half's addresses from a copy: equal ones would be kept from the first)
+        const lds_cptr qk = keep(pk), qv0 = keep(pv0), qv1 = keep(pv1), to_k = keep(uk), to_v = keep(uv);
+        auto issue = [&](auto o_) {
+          constexpr int o = decltype(o_)::value;
+          if constexpr (o < NF) {
+            r1_issue<(o / NKS) * 64 * D>(flip_bits(o < NKS ? pk : qk, (o % NKS) << 5), kf[o]);
+          } else if constexpr (o < NF + NV) {
+            constexpr int p = o - NF;
+            tr1_issue<(p / NDB) * 32 * D>(flip_bits(p < 2 * NDB ? pv0 : qv0, (p % NDB) << 6), vf[p][0]);
+            tr1_issue<(p / NDB) * 32 * D>(flip_bits(p < 2 * NDB ? pv1 : qv1, (p % NDB) << 6), vf[p][1]);
           }
-          float mx = sacc[0][0];
+        };
+        constexpr auto later = [](int o) {                   // LDS reads issued behind fragment o's when it is used
+          int n = 0;
+          for (int i = o + 1; i < o + kAhead && i < NF + NV; ++i) n += i < NF ? 1 : 2;
+          return n;
+        };
+        unsigned pf[2][8];
+        float sum[2], y = 0.f;
+        float ref = 0.f;
+        auto probability = [&](auto kb_, const floatx16& s, int e) {
+          constexpr int kb = decltype(kb_)::value;
+          const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref));
+          sum[kb] = e == 0 ? z : sum[kb] + z;
+          if (e & 1) {
+            typedef float float2v __attribute__((ext_vector_type(2)));
+            unsigned w = __builtin_bit_cast(unsigned, __builtin_convertvector((float2v){y, z}, bf16x2v));
+            asm volatile("" : "+v"(w));                      // (packed here: not the two floats kept)
+            pf[kb][e >> 1] = w;
+          }
+          y = z;
+        };
+        // The half's reference: it moves (rarely) where a lane's sum gets large, and from -inf at the first key that is seen; the half's scores and
+        // probabilities are formed again.  (Scores kept for this case would cost registers in every tile.)
+        auto settle = [&](auto kb_) {
+          constexpr int kb = decltype(kb_)::value;
+          if (__builtin_expect(__any(!(sum[kb] <= kLazySum) || m == -INFINITY), 0)) {
+            floatx16 s;
+            const lds_cptr again = keep(pk);
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+            for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[kb][r]);
-          mx = fmaxf(mx, xor32(mx)) * a.scale_log2;
-          if (__any(mx > m + kLazy)) {
+            for (int ks = 0; ks < NKS; ++ks)
+              s = mfma32(*(LDS_PTR(const bf16x8))(flip_bits(again, ks << 5) + kb * 64 * D), qf[ks], s);
+            if (masked) mask(s, kb);
+            float mx = s[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+            mx = fmaxf(mx, xor32(mx)) * a.scale_log2;
             const float to_m = fmaxf(m, mx), alpha = to_m == m ? 1.f : __builtin_amdgcn_exp2f(m - to_m);
             m = to_m;
             l *= alpha;
@@ -314,76 +358,111 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a
             for (int db = 0; db < NDB; ++db)
 #pragma unroll
               for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+            ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) probability(kb_, s, e);
           }
-          const float ref = m == -INFINITY ? 0.f : m;        // nothing seen yet: every score is -inf
-          bf16x8 pf[4];
-          float sum[4];
+          l += sum[kb];
+        };
+        auto weights = [&](int j) {
+          typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+          const unsigned* w = &pf[j >> 1][4 * (j & 1)];
+          return __builtin_bit_cast(bf16x8, (uint4v){w[0], w[1], w[2], w[3]});
+        };
+        // probabilities beside product i of NKS: not beside the first two, whose scores are still on their way
+        auto share = [&](auto kb_, auto i_) {
+          constexpr int i = decltype(i_)::value;
+          if constexpr (i >= 2) static_for<(i - 2) * 16 / (NKS - 2), (i - 1) * 16 / (NKS - 2)>([&](auto e_) { probability(kb_, sacc[decltype(kb_)::value], decltype(e_)::value); });
+        };
+        const Scales<D> sc = piece_scales<D>(x, k0 + kKeys, visible);
+        bf16x4 part;
+        static_for<0, kAhead>([&](auto o_) { issue(o_); });
+        static_for<0, NKS>([&](auto i_) {
+          constexpr int i = decltype(i_)::value;
+          wait_frag<later(i)>(kf[i]);
+          sacc[0] = mfma32(kf[i], qf[i], sacc[0]);
+          issue(IC<i + kAhead>{});
+          unpack_slot<D>(x, to_k, to_v, i, sc, part);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if (masked) mask(sacc[0], 0);
+        ref = m == -INFINITY ? 0.f : m;
+        static_for<0, NKS>([&](auto i_) {
+          constexpr int i = decltype(i_)::value, o = NKS + i;
+          wait_frag<later(o)>(kf[o]);
+          sacc[1] = mfma32(kf[o], qf[i], sacc[1]);
+          issue(IC<o + kAhead>{});
+          share(IC<0>{}, i_);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        settle(IC<0>{});
+        if (masked) mask(sacc[1], 1);
+        static_for<0, 2 * NDB>([&](auto i_) {
+          constexpr int i = decltype(i_)::value;
+          wait_frag<later(NF + i)>(vf[i][0], vf[i][1]);
+          oacc[i % NDB] = mfma32(join_frag(vf[i][0], vf[i][1]), weights(i / NDB), oacc[i % NDB]);
+          issue(IC<NF + i + kAhead>{});
+          share(IC<1>{}, i_);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        settle(IC<1>{});
+        LDS_PTR(const int) info = (LDS_PTR(const int))(lds + kBadAt<D> + buf * kBadBytes);
+        const int any_bad = info[0] | info[1] | info[2] | info[3];
+        static_for<0, 2 * NDB>([&](auto i_) {
+          constexpr int i = decltype(i_)::value, p = 2 * NDB + i;
+          wait_frag<later(NF + p)>(vf[p][0], vf[p][1]);
+          oacc[i % NDB] = mfma32(join_frag(vf[p][0], vf[p][1]), weights(2 + i / NDB), oacc[i % NDB]);
+          issue(IC<NF + p + kAhead>{});
+          unpack_slot<D>(x, to_k, to_v, NKS + i, sc, part);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        note_bad<D>(lds, buf ^ 1, sc.bad);
+        if (__builtin_amdgcn_readfirstlane(any_bad)) {       // scales that are not finite: NaN where their keys are seen
+          int hit = 0;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            sum[j] = 0.f;
+          for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int r = 8 * (j & 1) + i;
-              sacc[j >> 1][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[j >> 1][r], a.scale_log2, -ref));
-              sum[j] += sacc[j >> 1][r];
+            for (int r = 0; r < 16; ++r) {
+              const int key = 32 * kb + 8 * (r >> 2) + 4 * half + (r & 3), chunk = 2 * kb + (r >> 3);
+              hit |= info[chunk] && k0 + key <= limit ? info[4 + key] : 0;
             }
-            pf[j] = pack8(sacc[j >> 1], 8 * (j & 1));
-          }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          // O^T += V^T P^T: one batch of four V^T fragments (the four 16-key steps) per block of 32 channels
-          Tr4 tb[NDB];
-          constexpr int kRows = 32 * D;
-          tr4_issue<0, kRows, 2 * kRows, 3 * kRows>(pv0, pv1, tb[0]);
+          hit |= __shfl_xor(hit, 32);
 #pragma unroll
           for (int db = 0; db < NDB; ++db) {
-            if (db + 1 < NDB) tr4_issue_wait<0, kRows, 2 * kRows, 3 * kRows>(flip_bits(pv0, (db + 1) << 6), flip_bits(pv1, (db + 1) << 6), tb[db + 1], tb[db]);
-            else tr4_wait(tb[db]);
+            const float poison = hit & (256 | 1 << db) ? __builtin_nanf("") : 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) oacc[db] = mfma32(tr4_frag(tb[db], j), pf[j], oacc[db]);
+            for (int r = 0; r < 16; ++r) oacc[db][r] += poison;
           }
-          if (some & 2) {                                    // a value scale that is not finite: NaN where its key is seen
-            int hit = 0;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const int chunk = 2 * kb + (r >> 3), ci = chunk == 0 ? i0 : chunk == 1 ? i1 : chunk == 2 ? i2 : i3;
-                const int groups = info[4 + 32 * kb + 8 * (r >> 2) + 4 * half + (r & 3)];
-                hit |= (ci & 2) != 0 & sacc[kb][r] != 0.f ? groups : 0;
-              }
-            hit |= __shfl_xor(hit, 32);
-#pragma unroll
-            for (int db = 0; db < NDB; ++db) {
-              const float poison = hit >> db & 1 ? __builtin_nanf("") : 0.f;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) oacc[db][r] += poison;
-            }
-          }
-        } else {                                             // nothing that this wave's columns see: only fetch
-          note_stage<D>(x, lds, buf ^ 1, unpack_stage<D>(x, uk, uv, k0 + kKeys, visible));
+          l += hit & 256 ? __builtin_nanf("") : 0.f;
         }
+      };
+      for (int k0 = k_begin; k0 < k_end; k0 += kKeys, buf ^= 1) {
+        // (The last tiles load and unpack again what nobody reads: no branch between the products.)
+        if (k0 < wave_end) products(k0);
+        else unpack_stage<D>(x, lds, buf ^ 1, uk, uv, k0 + kKeys, visible);   // nothing that this wave's columns see
+        there = x.there;
         const int entry_now = entry;                         // (one place for both ways: a copy of what is loaded would wait for it)
-        entry = load_entry(a.c, table, k0 + 4 * kKeys, k_end);   // (first: loads complete in order)
-        load_stage<D>(x, a.c, piece, pb, entry_now, k0 + 3 * kKeys, k_end);
-        constexpr int to_other = buf ? -2 * kTileBytes<D> : 2 * kTileBytes<D>;
+        entry = load_entry(a.c, table, k0 + 3 * kKeys, k_end);   // (first: loads complete in order)
+        load_stage<D>(x, a.c, piece, pb, entry_now, k0 + 2 * kKeys, k_end);
+        const int to_other = buf ? -2 * kTileBytes<D> : 2 * kTileBytes<D>;
         pk += to_other; pv0 += to_other; pv1 += to_other;
         uk -= to_other; uv -= to_other;
         // this tile's reads and the next one's writes are done (loads on their way may stay so)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-      };
-      for (int k0 = k_begin; k0 < k_end; k0 += 2 * kKeys) {
-        tile(IC<0>{}, xb, k0);
-        if (k0 + kKeys < k_end) tile(IC<1>{}, xa, k0 + kKeys);
       }
     }
 
     l += xor32(l);
+    // (the column again, from a copy of the thread's number: its places in the outputs would otherwise be kept in registers through the walk)
+    const int me = thread_number();
+    const int out_half = me >> 5 & 1, out_col = (me >> 6) * 32 + (me & 31), out_row = row_first + (in_row + out_col) / a.group,
+              out_head = hk * a.group + (in_row + out_col) % a.group;
     if (first && last) {
-      if (real) {
+      if (out_col < cols) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        bf16* op = o + ((size_t)(s.row0 + row) * a.Hq + head) * D + 4 * half;
+        bf16* op = o + ((size_t)(s.row0 + out_row) * a.Hq + out_head) * D + 4 * out_half;
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -392,17 +471,17 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a
                                 l == 0.f ? 0.f : oacc[db][r + 3] * inv};
             store_out<4>(op + 32 * db + 2 * r, x);
           }
-        if (lse && half == 0) lse[(size_t)head * a.c.n_rows + s.row0 + row] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+        if (lse && out_half == 0) lse[(size_t)out_head * a.c.n_rows + s.row0 + out_row] = (m + __builtin_amdgcn_logf(l)) * kLn2;
       }
     } else {
       float* part = part_of<D>(ws + parts_at, id, first ? 1 : 0);
-      if (real) {
+      if (out_col < cols) {
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; r += 4)
-            *reinterpret_cast<floatx4v*>(part + mine * D + 32 * db + 2 * r + 4 * half) = floatx4v{oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]};
-        if (half == 0) { part[kCols * D + mine] = m; part[kCols * D + kCols + mine] = l; }
+            *reinterpret_cast<floatx4v*>(part + out_col * D + 32 * db + 2 * r + 4 * out_half) = floatx4v{oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]};
+        if (out_half == 0) { part[kCols * D + out_col] = m; part[kCols * D + kCols + out_col] = l; }
       }
     }
     if (first) {
