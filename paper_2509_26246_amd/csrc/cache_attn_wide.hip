@@ -20,7 +20,7 @@
 namespace slimattn {
 namespace {
 
-constexpr int kCols = 128;           // query columns of a block, 32 per wave
+constexpr int kCols = 256;           // query columns of a block: two groups of 32 per wave
 constexpr int kKeys = 64;            // keys of a tile
 constexpr int kFixedKeys = 192;      // what an item costs beside its keys (its queries, its output), in keys
 constexpr int kLeastKeys = 256;      // work that is worth a block and its parts
@@ -203,13 +203,35 @@ __device__ __forceinline__ void wait_frag(bf16x8& f) { asm volatile("s_waitcnt l
 template <int N>
 __device__ __forceinline__ void wait_frag(short4v& a, short4v& b) { asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "n"(N)); }
 
+// acc += a b, the accumulator in the accumulation registers (there are no others left for it): from inline asm, whose results and operands the
+// compiler does not time.  Results are read by later products on the same accumulator or behind rest(); b and acc are written well ahead, or in
+// front of rest_writes().
+__device__ __forceinline__ void mfma_acc(floatx16& acc, bf16x8 a, bf16x8 b) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+template <int N>
+__device__ __forceinline__ void rest(floatx16 (&acc)[2][N]) {
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int db = 0; db < N; ++db) asm volatile("s_nop 15" : "+a"(acc[g][db]));
+  asm volatile("s_nop 15\n\ts_nop 15");
+}
+template <int N>
+__device__ __forceinline__ void rest_writes(floatx16 (&acc)[2][N]) {
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int db = 0; db < N; ++db) asm volatile("s_nop 7" : "+a"(acc[g][db]));
+}
+
 __device__ __forceinline__ bf16x8 join_frag(short4v a, short4v b) {
   typedef __attribute__((__vector_size__(8 * sizeof(short)))) short short8v;
   return __builtin_bit_cast(bf16x8, (short8v)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a, const bf16* __restrict__ q, const char* __restrict__ cache, bf16* __restrict__ o,
+__global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a, const bf16* __restrict__ q, const char* __restrict__ cache, bf16* __restrict__ o,
                                                                       float* __restrict__ lse, char* __restrict__ ws, size_t parts_at) {
   constexpr int NKS = D / 16, NDB = D / 32;
   __shared__ __attribute__((aligned(1024))) char smem[kLdsBytes<D>];
@@ -241,69 +263,74 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a
     const long long col0 = (long long)t * kCols;             // columns of a sequence: rows * group may pass 32 bits
     const int cols = (int)min((long long)s.rows * a.group - col0, (long long)kCols);
     const int base = s.len - s.rows, row_first = (int)(col0 / a.group), in_row = (int)(col0 % a.group);
-    const int mine = wave * 32 + l32, row = row_first + (in_row + mine) / a.group, head = hk * a.group + (in_row + mine) % a.group;
-    const bool real = mine < cols;
-    const int limit = real ? base + row : -1;
     const int visible = base + row_first + (in_row + cols - 1) / a.group + 1;
-    const int wave_all = base + row_first + (in_row + wave * 32) / a.group + 1;                 // keys that all of the wave's columns see
-    const int wave_end = wave * 32 < cols ? base + row_first + (in_row + min(wave * 32 + 31, cols - 1)) / a.group + 1 : 0;
+    const int wave_all = base + row_first + (in_row + wave * 64) / a.group + 1;                 // keys that all of the wave's columns see
     const int k_begin = first ? 0 : __builtin_amdgcn_readfirstlane(s.keys_at(from));
     const int k_end = __builtin_amdgcn_readfirstlane(last ? visible : min(s.keys_at(to), visible));
 
-    bf16x8 qf[NKS];
-    {
+    bf16x8 qf[2][NKS];
+    int limit[2];                                            // last key that the lane's columns see
+    float m[2], l[2];                                        // their references (log2 units), their sums against them
+    floatx16 oacc[2][NDB];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int mine = wave * 64 + 32 * g + l32, row = row_first + (in_row + mine) / a.group, head = hk * a.group + (in_row + mine) % a.group;
+      const bool real = mine < cols;
       const bf16* qp = q + ((size_t)(s.row0 + (real ? row : 0)) * a.Hq + (real ? head : 0)) * D + 8 * half;
       const unsigned flip = a.q_sign < 0.f ? 0x80008000u : 0u, keep = real && a.q_sign != 0.f ? 0xffffffffu : 0u;
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks) {
         uint4 w = *reinterpret_cast<const uint4*>(qp + 16 * ks);
         w.x = (w.x ^ flip) & keep; w.y = (w.y ^ flip) & keep; w.z = (w.z ^ flip) & keep; w.w = (w.w ^ flip) & keep;
-        qf[ks] = __builtin_bit_cast(bf16x8, w);
+        qf[g][ks] = __builtin_bit_cast(bf16x8, w);
+      }
+      limit[g] = real ? base + row - 4 * half : -64;         // less what the lane's half adds to a key's number
+      m[g] = real ? -INFINITY : 0.f;
+      l[g] = 0.f;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[g][db][r] = 0.f;
+        asm volatile("" : "+a"(oacc[g][db]));
       }
     }
-    floatx16 oacc[NDB];
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
-    float m = real ? -INFINITY : 0.f, l = 0.f;               // the reference (log2 units), the sum against it
+    rest_writes(oacc);
 
     const int32_t* table = a.c.table + (size_t)b * a.c.max_pages;
     const char* piece = cache + hk * head_bytes<D>(a.c);
     const unsigned pb = (unsigned)page_bytes<D>(a.c);
     if (k_begin < k_end) {
-      Stage<D> x;                                            // the next tile, on its way
-      const int e0 = load_entry(a.c, table, k_begin, k_end), e1 = load_entry(a.c, table, k_begin + kKeys, k_end);
-      int entry = load_entry(a.c, table, k_begin + 2 * kKeys, k_end);
-      load_stage<D>(x, a.c, piece, pb, e0, k_begin, k_end);
+      // two tiles on their way beside the one at hand
+      Stage<D> xa, xb;
+      const int e0 = load_entry(a.c, table, k_begin, k_end), e1 = load_entry(a.c, table, k_begin + kKeys, k_end), e2 = load_entry(a.c, table, k_begin + 2 * kKeys, k_end);
+      int entry = load_entry(a.c, table, k_begin + 3 * kKeys, k_end);
+      load_stage<D>(xa, a.c, piece, pb, e0, k_begin, k_end);
+      load_stage<D>(xb, a.c, piece, pb, e1, k_begin + kKeys, k_end);
       __syncthreads();                                       // the buffers are free
-      unpack_stage<D>(x, lds, 0, lds + unpack_keys_at<D>(), lds + unpack_values_at<D>(), k_begin, visible);
-      int there = x.there, buf = 0;
-      load_stage<D>(x, a.c, piece, pb, e1, k_begin + kKeys, k_end);
+      unpack_stage<D>(xa, lds, 0, lds + unpack_keys_at<D>(), lds + unpack_values_at<D>(), k_begin, visible);
+      int there = xa.there;
+      load_stage<D>(xa, a.c, piece, pb, e2, k_begin + 2 * kKeys, k_end);
       __syncthreads();
       lds_cptr pk = lds_row_ptr<D>(lds, l32, 8 * half), pv0, pv1;   // this buffer's fragments; the other's unpacked pieces
       lds_tr_ptrs<D>(lds + kTileBytes<D>, 0, lane, pv0, pv1);
       lds_cptr uk = keep(lds + 2 * kTileBytes<D> + unpack_keys_at<D>()), uv = keep(lds + 2 * kTileBytes<D> + unpack_values_at<D>());
 
-      // The products of tile k0, and between them the other work: x, the next tile, is unpacked beside the first half's scores and the
-      // second half's O^T products; a half's probabilities are formed beside the products that follow its scores.  A half is 32 keys.
-      // Fragments are read kAhead products ahead.  
-      auto products = [&](const int k0) {
-        constexpr int NF = 2 * NKS, NV = 4 * NDB, kAhead = 4;
-        const int limit_here = limit - (thread_number() >> 3 & 4);
+      // The products of tile k0 in buffer BUF, and between them the other work: x, the next tile, is unpacked beside the first half's scores and the
+      // second half's O^T products; a half's probabilities are formed beside the products that follow its scores.  A half is 32 keys.  A
+      // fragment serves both groups of columns; fragments are read kAhead ahead of their products.
+      auto tile = [&](auto buf_, Stage<D>& x, const int k0) {
+        constexpr int BUF = decltype(buf_)::value, NF = 2 * NKS, NV = 4 * NDB, kAhead = 3;
         const bool masked = there != 15 || k0 + kKeys > wave_all;
-        auto mask = [&](floatx16& s, int kb) {               // key 32 kb + 8 (r / 4) + 4 half + r % 4 of the tile
+        auto mask = [&](floatx16& s, int kb, int g) {        // key 32 kb + 8 (r / 4) + 4 half + r % 4 of the tile
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (32 * kb + 8 * (r >> 2) + (r & 3) > limit_here - k0 || !(there >> (2 * kb + (r >> 3)) & 1)) s[r] = -INFINITY;
+            if (32 * kb + 8 * (r >> 2) + (r & 3) > limit[g] - k0 || !(there >> (2 * kb + (r >> 3)) & 1)) s[r] = -INFINITY;
         };
-        floatx16 sacc[2];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[0][r] = sacc[1][r] = 0.f;
+        floatx16 sacc[2][2];                                 // [half][group]
         bf16x8 kf[NF];
         short4v vf[NV][2];
         // (the second half's addresses from a copy: equal ones would be kept from the first)
-        const lds_cptr qk = keep(pk), qv0 = keep(pv0), qv1 = keep(pv1), to_k = keep(uk), to_v = keep(uv);
+        const lds_cptr qk = keep(pk), qv0 = keep(pv0), qv1 = keep(pv1);
         auto issue = [&](auto o_) {
           constexpr int o = decltype(o_)::value;
           if constexpr (o < NF) {
@@ -319,169 +346,205 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a
           for (int i = o + 1; i < o + kAhead && i < NF + NV; ++i) n += i < NF ? 1 : 2;
           return n;
         };
-        unsigned pf[2][8];
-        float sum[2], y = 0.f;
-        float ref = 0.f;
-        auto probability = [&](auto kb_, const floatx16& s, int e) {
+        unsigned pf[2][2][8];
+        float sum[2], y[2], ref[2];
+        auto probability = [&](auto kb_, int g, const floatx16& s, int e) {
           constexpr int kb = decltype(kb_)::value;
-          const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref));
-          sum[kb] = e == 0 ? z : sum[kb] + z;
+          const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref[g]));
+          sum[g] = e == 0 ? z : sum[g] + z;
           if (e & 1) {
             typedef float float2v __attribute__((ext_vector_type(2)));
-            unsigned w = __builtin_bit_cast(unsigned, __builtin_convertvector((float2v){y, z}, bf16x2v));
+            unsigned w = __builtin_bit_cast(unsigned, __builtin_convertvector((float2v){y[g], z}, bf16x2v));
             asm volatile("" : "+v"(w));                      // (packed here: not the two floats kept)
-            pf[kb][e >> 1] = w;
+            pf[kb][g][e >> 1] = w;
           }
-          y = z;
+          y[g] = z;
         };
-        // The half's reference: it moves (rarely) where a lane's sum gets large, and from -inf at the first key that is seen; the half's scores and
+        // A half's references: they move (rarely) where a lane's sum gets large, and from -inf at the first key that is seen; the half's scores and
         // probabilities are formed again.  (Scores kept for this case would cost registers in every tile.)
         auto settle = [&](auto kb_) {
           constexpr int kb = decltype(kb_)::value;
-          if (__builtin_expect(__any(!(sum[kb] <= kLazySum) || m == -INFINITY), 0)) {
-            floatx16 s;
+          const bool moves = !(fmaxf(sum[0], sum[1]) <= kLazySum) || sum[0] != sum[0] || sum[1] != sum[1] || fminf(m[0], m[1]) == -INFINITY;
+          if (__builtin_expect(__any(moves), 0)) {
             const lds_cptr again = keep(pk);
+            rest(oacc);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = 0.f;
+            for (int g = 0; g < 2; ++g) {
+              floatx16 s;
 #pragma unroll
-            for (int ks = 0; ks < NKS; ++ks)
-              s = mfma32(*(LDS_PTR(const bf16x8))(flip_bits(again, ks << 5) + kb * 64 * D), qf[ks], s);
-            if (masked) mask(s, kb);
-            float mx = s[0];
+              for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-            mx = fmaxf(mx, xor32(mx)) * a.scale_log2;
-            const float to_m = fmaxf(m, mx), alpha = to_m == m ? 1.f : __builtin_amdgcn_exp2f(m - to_m);
-            m = to_m;
-            l *= alpha;
+              for (int ks = 0; ks < NKS; ++ks)
+                s = mfma32(*(LDS_PTR(const bf16x8))(flip_bits(again, ks << 5) + kb * 64 * D), qf[g][ks], s);
+              if (masked) mask(s, kb, g);
+              float mx = s[0];
 #pragma unroll
-            for (int db = 0; db < NDB; ++db)
+              for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+              mx = fmaxf(mx, xor32(mx)) * a.scale_log2;
+              const float to_m = fmaxf(m[g], mx), alpha = to_m == m[g] ? 1.f : __builtin_amdgcn_exp2f(m[g] - to_m);
+              m[g] = to_m;
+              l[g] *= alpha;
 #pragma unroll
-              for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
-            ref = m == -INFINITY ? 0.f : m;
+              for (int db = 0; db < NDB; ++db)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) probability(kb_, s, e);
+                for (int r = 0; r < 16; ++r) oacc[g][db][r] *= alpha;
+              ref[g] = m[g] == -INFINITY ? 0.f : m[g];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) probability(kb_, g, s, e);
+            }
+            rest_writes(oacc);
           }
-          l += sum[kb];
+          l[0] += sum[0];
+          l[1] += sum[1];
         };
-        auto weights = [&](int j) {
+        auto weights = [&](int j, int g) {
           typedef unsigned uint4v __attribute__((ext_vector_type(4)));
-          const unsigned* w = &pf[j >> 1][4 * (j & 1)];
+          const unsigned* w = &pf[j >> 1][g][4 * (j & 1)];
           return __builtin_bit_cast(bf16x8, (uint4v){w[0], w[1], w[2], w[3]});
         };
-        // probabilities beside product i of NKS: not beside the first two, whose scores are still on their way
+        // a half's 32 probabilities beside products 2 .. 2 NKS - 1 (the scores are still on their way beside the first two)
         auto share = [&](auto kb_, auto i_) {
-          constexpr int i = decltype(i_)::value;
-          if constexpr (i >= 2) static_for<(i - 2) * 16 / (NKS - 2), (i - 1) * 16 / (NKS - 2)>([&](auto e_) { probability(kb_, sacc[decltype(kb_)::value], decltype(e_)::value); });
+          constexpr int i = decltype(i_)::value, n = 2 * NKS - 2;
+          if constexpr (i >= 2)
+            static_for<(i - 2) * 32 / n, (i - 1) * 32 / n>([&](auto e_) {
+              constexpr int e = decltype(e_)::value;
+              probability(kb_, e & 1, sacc[decltype(kb_)::value][e & 1], e >> 1);
+            });
         };
         const Scales<D> sc = piece_scales<D>(x, k0 + kKeys, visible);
         bf16x4 part;
         static_for<0, kAhead>([&](auto o_) { issue(o_); });
-        static_for<0, NKS>([&](auto i_) {
-          constexpr int i = decltype(i_)::value;
-          wait_frag<later(i)>(kf[i]);
-          sacc[0] = mfma32(kf[i], qf[i], sacc[0]);
-          issue(IC<i + kAhead>{});
-          unpack_slot<D>(x, to_k, to_v, i, sc, part);
+        static_for<0, 2 * NKS>([&](auto i_) {
+          constexpr int i = decltype(i_)::value, ks = i / 2, g = i % 2;
+          if constexpr (g == 0) wait_frag<later(ks)>(kf[ks]);
+          if constexpr (ks == 0) {
+            const floatx16 zero = {};
+            sacc[0][g] = mfma32(kf[ks], qf[g][ks], zero);
+          } else {
+            sacc[0][g] = mfma32(kf[ks], qf[g][ks], sacc[0][g]);
+          }
+          if constexpr (g == 1) issue(IC<ks + kAhead>{});
+          else unpack_slot<D>(x, uk, uv, ks, sc, part);
           __builtin_amdgcn_sched_barrier(0);
         });
-        if (masked) mask(sacc[0], 0);
-        ref = m == -INFINITY ? 0.f : m;
-        static_for<0, NKS>([&](auto i_) {
-          constexpr int i = decltype(i_)::value, o = NKS + i;
-          wait_frag<later(o)>(kf[o]);
-          sacc[1] = mfma32(kf[o], qf[i], sacc[1]);
-          issue(IC<o + kAhead>{});
+        if (masked) {
+          mask(sacc[0][0], 0, 0);
+          mask(sacc[0][1], 0, 1);
+        }
+        ref[0] = m[0] == -INFINITY ? 0.f : m[0];
+        ref[1] = m[1] == -INFINITY ? 0.f : m[1];
+        static_for<0, 2 * NKS>([&](auto i_) {
+          constexpr int i = decltype(i_)::value, ks = i / 2, g = i % 2, o = NKS + ks;
+          if constexpr (g == 0) wait_frag<later(o)>(kf[o]);
+          if constexpr (ks == 0) {
+            const floatx16 zero = {};
+            sacc[1][g] = mfma32(kf[o], qf[g][ks], zero);
+          } else {
+            sacc[1][g] = mfma32(kf[o], qf[g][ks], sacc[1][g]);
+          }
+          if constexpr (g == 1) issue(IC<o + kAhead>{});
           share(IC<0>{}, i_);
           __builtin_amdgcn_sched_barrier(0);
         });
         settle(IC<0>{});
-        if (masked) mask(sacc[1], 1);
-        static_for<0, 2 * NDB>([&](auto i_) {
-          constexpr int i = decltype(i_)::value;
-          wait_frag<later(NF + i)>(vf[i][0], vf[i][1]);
-          oacc[i % NDB] = mfma32(join_frag(vf[i][0], vf[i][1]), weights(i / NDB), oacc[i % NDB]);
-          issue(IC<NF + i + kAhead>{});
+        if (masked) {
+          mask(sacc[1][0], 1, 0);
+          mask(sacc[1][1], 1, 1);
+        }
+        asm volatile("s_nop 7");                             // the last probabilities are written: see mfma_acc
+        static_for<0, 4 * NDB>([&](auto i_) {
+          constexpr int i = decltype(i_)::value, p = i / 2, g = i % 2;
+          if constexpr (g == 0) wait_frag<later(NF + p)>(vf[p][0], vf[p][1]);
+          mfma_acc(oacc[g][p % NDB], join_frag(vf[p][0], vf[p][1]), weights(p / NDB, g));
+          if constexpr (g == 1) issue(IC<NF + p + kAhead>{});
           share(IC<1>{}, i_);
           __builtin_amdgcn_sched_barrier(0);
         });
         settle(IC<1>{});
-        LDS_PTR(const int) info = (LDS_PTR(const int))(lds + kBadAt<D> + buf * kBadBytes);
+        LDS_PTR(const int) info = (LDS_PTR(const int))(lds + kBadAt<D> + BUF * kBadBytes);
         const int any_bad = info[0] | info[1] | info[2] | info[3];
-        static_for<0, 2 * NDB>([&](auto i_) {
-          constexpr int i = decltype(i_)::value, p = 2 * NDB + i;
-          wait_frag<later(NF + p)>(vf[p][0], vf[p][1]);
-          oacc[i % NDB] = mfma32(join_frag(vf[p][0], vf[p][1]), weights(2 + i / NDB), oacc[i % NDB]);
-          issue(IC<NF + p + kAhead>{});
-          unpack_slot<D>(x, to_k, to_v, NKS + i, sc, part);
+        asm volatile("s_nop 7");
+        static_for<0, 4 * NDB>([&](auto i_) {
+          constexpr int i = decltype(i_)::value, p = 2 * NDB + i / 2, g = i % 2;
+          if constexpr (g == 0) wait_frag<later(NF + p)>(vf[p][0], vf[p][1]);
+          mfma_acc(oacc[g][p % NDB], join_frag(vf[p][0], vf[p][1]), weights(p / NDB, g));
+          if constexpr (g == 1) issue(IC<NF + p + kAhead>{});
+          else unpack_slot<D>(x, uk, uv, NKS + i / 2, sc, part);
           __builtin_amdgcn_sched_barrier(0);
         });
-        note_bad<D>(lds, buf ^ 1, sc.bad);
+        note_bad<D>(lds, BUF ^ 1, sc.bad);
         if (__builtin_amdgcn_readfirstlane(any_bad)) {       // scales that are not finite: NaN where their keys are seen
-          int hit = 0;
+          rest(oacc);
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+          for (int g = 0; g < 2; ++g) {
+            int hit = 0;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int key = 32 * kb + 8 * (r >> 2) + 4 * half + (r & 3), chunk = 2 * kb + (r >> 3);
-              hit |= info[chunk] && k0 + key <= limit ? info[4 + key] : 0;
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int key = 32 * kb + 8 * (r >> 2) + (r & 3), chunk = 2 * kb + (r >> 3);
+                hit |= info[chunk] && k0 + key <= limit[g] ? info[4 + key + 4 * half] : 0;
+              }
+            hit |= __shfl_xor(hit, 32);
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) {
+              const float poison = hit & (256 | 1 << db) ? __builtin_nanf("") : 0.f;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) oacc[g][db][r] += poison;
             }
-          hit |= __shfl_xor(hit, 32);
-#pragma unroll
-          for (int db = 0; db < NDB; ++db) {
-            const float poison = hit & (256 | 1 << db) ? __builtin_nanf("") : 0.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) oacc[db][r] += poison;
+            l[g] += hit & 256 ? __builtin_nanf("") : 0.f;
           }
-          l += hit & 256 ? __builtin_nanf("") : 0.f;
+          rest_writes(oacc);
         }
-      };
-      for (int k0 = k_begin; k0 < k_end; k0 += kKeys, buf ^= 1) {
-        // (The last tiles load and unpack again what nobody reads: no branch between the products.)
-        if (k0 < wave_end) products(k0);
-        else unpack_stage<D>(x, lds, buf ^ 1, uk, uv, k0 + kKeys, visible);   // nothing that this wave's columns see
         there = x.there;
-        const int entry_now = entry;                         // (one place for both ways: a copy of what is loaded would wait for it)
-        entry = load_entry(a.c, table, k0 + 3 * kKeys, k_end);   // (first: loads complete in order)
-        load_stage<D>(x, a.c, piece, pb, entry_now, k0 + 2 * kKeys, k_end);
-        const int to_other = buf ? -2 * kTileBytes<D> : 2 * kTileBytes<D>;
+        const int entry_now = entry;
+        entry = load_entry(a.c, table, k0 + 4 * kKeys, k_end);   // (first: loads complete in order)
+        load_stage<D>(x, a.c, piece, pb, entry_now, k0 + 3 * kKeys, k_end);
+        constexpr int to_other = BUF ? -2 * kTileBytes<D> : 2 * kTileBytes<D>;
         pk += to_other; pv0 += to_other; pv1 += to_other;
         uk -= to_other; uv -= to_other;
         // this tile's reads and the next one's writes are done (loads on their way may stay so)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+      };
+      // (Tiles in pairs, without a branch: an odd number's last partner has no chunk in a page and adds nothing, and the last tiles load and unpack
+      // again what nobody reads.)
+      for (int k0 = k_begin; k0 < k_end; k0 += 2 * kKeys) {
+        tile(IC<0>{}, xb, k0);
+        tile(IC<1>{}, xa, k0 + kKeys);
       }
     }
+    rest(oacc);
 
-    l += xor32(l);
-    // (the column again, from a copy of the thread's number: its places in the outputs would otherwise be kept in registers through the walk)
-    const int me = thread_number();
-    const int out_half = me >> 5 & 1, out_col = (me >> 6) * 32 + (me & 31), out_row = row_first + (in_row + out_col) / a.group,
-              out_head = hk * a.group + (in_row + out_col) % a.group;
-    if (first && last) {
-      if (out_col < cols) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        bf16* op = o + ((size_t)(s.row0 + out_row) * a.Hq + out_head) * D + 4 * out_half;
+    // (the columns again, from a copy of the thread's number: their places in the outputs would otherwise be kept in registers through the walk)
+    const int me = thread_number(), out_half = me >> 5 & 1;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int col = (me >> 6) * 64 + 32 * g + (me & 31), row = row_first + (in_row + col) / a.group, head = hk * a.group + (in_row + col) % a.group;
+      const float total = l[g] + xor32(l[g]);
+      if (col >= cols) continue;
+      if (first && last) {
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        bf16* op = o + ((size_t)(s.row0 + row) * a.Hq + head) * D + 4 * out_half;
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; r += 4) {
-            const float x[4] = {l == 0.f ? 0.f : oacc[db][r] * inv, l == 0.f ? 0.f : oacc[db][r + 1] * inv, l == 0.f ? 0.f : oacc[db][r + 2] * inv,
-                                l == 0.f ? 0.f : oacc[db][r + 3] * inv};
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = total == 0.f ? 0.f : oacc[g][db][r + e] * inv;
             store_out<4>(op + 32 * db + 2 * r, x);
           }
-        if (lse && out_half == 0) lse[(size_t)out_head * a.c.n_rows + s.row0 + out_row] = (m + __builtin_amdgcn_logf(l)) * kLn2;
-      }
-    } else {
-      float* part = part_of<D>(ws + parts_at, id, first ? 1 : 0);
-      if (out_col < cols) {
+        if (lse && out_half == 0) lse[(size_t)head * a.c.n_rows + s.row0 + row] = (m[g] + __builtin_amdgcn_logf(total)) * kLn2;
+      } else {
+        float* part = part_of<D>(ws + parts_at, id, first ? 1 : 0);
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; r += 4)
-            *reinterpret_cast<floatx4v*>(part + out_col * D + 32 * db + 2 * r + 4 * out_half) = floatx4v{oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]};
-        if (out_half == 0) { part[kCols * D + out_col] = m; part[kCols * D + kCols + out_col] = l; }
+            *reinterpret_cast<floatx4v*>(part + col * D + 32 * db + 2 * r + 4 * out_half) = floatx4v{oacc[g][db][r], oacc[g][db][r + 1], oacc[g][db][r + 2], oacc[g][db][r + 3]};
+        if (out_half == 0) { part[kCols * D + col] = m[g]; part[kCols * D + kCols + col] = total; }
       }
     }
     if (first) {
@@ -529,11 +592,11 @@ __global__ __launch_bounds__(kThreads) void cache_attn_wide_join_kernel(AttnArgs
 long long most_items(const slimattn_cache_params& p, int n_q_heads) {
   return ((long long)p.n_rows * (n_q_heads / p.n_kv_heads) / kCols + p.n_seqs) * p.n_kv_heads;
 }
-// Two blocks per compute unit, fewer where there cannot be work for them.
+// A block per compute unit, fewer where there cannot be work for them.
 int grid_blocks(const slimattn_cache_params& p, int n_q_heads) {
   const long long items = most_items(p, n_q_heads), keys = (long long)p.max_pages * p.page_size + kFixedKeys + 1;
-  const long long most = items > 512 ? 512 : items * (keys / kLeastKeys + 1);
-  return (int)(most < 512 ? most : 512);
+  const long long most = items > 256 ? 256 : items * (keys / kLeastKeys + 1);
+  return (int)(most < 256 ? most : 256);
 }
 
 }  // namespace
