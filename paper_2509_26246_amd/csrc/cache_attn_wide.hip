@@ -122,57 +122,60 @@ __device__ __forceinline__ bf16x4 unpack4(unsigned w, bool hi, float s) {
 }
 
 // LDS: [buffer][K tile, V tile], then per buffer and wave whether its chunk of the tile has scales that are not finite, and which of a key's groups
-// those are (bits 0 .. G-1 values, 8 keys).
-template <int D> constexpr int kTileBytes = kKeys * D * 2;
-template <int D> constexpr int kBadAt = 4 * kTileBytes<D>;
+// those are (bits 0 .. G-1 values, 8 keys).  Rows are padded (K fragments: 16 lanes, rows one behind the other, take 16 bytes each; V^T fragments: 16 lanes
+// take 4 rows x 32 bytes), so that every fragment is one lane address and a constant.
+template <int D> constexpr int kKRow = D * 2 + 16;
+template <int D> constexpr int kVRow = D * 2 + 32;
+template <int D> constexpr int kBuffer = kKeys * (kKRow<D> + kVRow<D>);
+template <int D> constexpr int kBadAt = 2 * kBuffer<D>;
 constexpr int kBadBytes = 16 + kKeys * 4;
 template <int D> constexpr int kLdsBytes = kBadAt<D> + 2 * kBadBytes;
 
-// The swizzle of a tile (lds_off16) is an exclusive or on address bits 4 to 7, and tiles begin at multiples of 256 bytes: what changes with a fragment's
-// column is an exclusive or with a constant, so one address register serves them all.
-__device__ __forceinline__ lds_cptr flip_bits(lds_cptr p, int bits) { return (lds_cptr)(unsigned)((unsigned)(uintptr_t)p ^ bits); }
+// Where this thread's pieces of a tile go in a buffer: its first K word (channels 8 j ..; word g 64 bytes further each) and its first V word
+// (channels 8 j G ..; word i 16 bytes further each).
+template <int D>
+__device__ __forceinline__ int unpack_keys_at(int tid) { return (tid >> 2) * kKRow<D> + (tid & 3) * 16; }
+template <int D>
+__device__ __forceinline__ int unpack_values_at(int tid) { return kKeys * kKRow<D> + (tid >> 2) * kVRow<D> + (tid & 3) * (D / 32) * 16; }
 
-// Where this thread's pieces of a tile go in a buffer: its first K word (channels 8 j ..; word g: address bits g << 6 flipped) and its first V word
-// (channels 8 j G ..; word i: i << 4).
+// Makes the scales of this thread's piece fit for products.  Chunks without a page and keys from `end` on (behind the last that some column of the
+// block sees) may hold anything: their scales become zeros, and the softmax masks them.  So do scales that are not finite, which only columns
+// that see their key may notice: the bits of those (note_bad; the softmax makes NaN of them for those columns).
 template <int D>
-__device__ __forceinline__ int unpack_keys_at() { return lds_off16<D>(threadIdx.x >> 2, threadIdx.x & 3); }
-template <int D>
-__device__ __forceinline__ int unpack_values_at() { return kTileBytes<D> + lds_off16<D>(threadIdx.x >> 2, (threadIdx.x & 3) * (D / 32)); }
-// The scales of this thread's piece, those of its keys per group, then its values'.  Chunks without a page and keys from `end` on (behind the last that
-// some column of the block sees) may hold anything: their scales become zeros, and the softmax masks them.  So do scales that are not
-// finite, which only columns that see their key may notice: bad (note_bad; the softmax makes NaN of them for those columns).
-template <int D>
-struct Scales { float k[D / 32], v; int bad; };
-template <int D>
-__device__ __forceinline__ Scales<D> piece_scales(const Stage<D>& x, int k0, int end) {
+__device__ __forceinline__ int clean_scales(Stage<D>& x, int k0, int end) {
   constexpr int G = D / 32;
   const int tid = thread_number(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool seen = (x.there >> wave & 1) && k0 + (tid >> 2) < end;
-  Scales<D> s;
-  s.bad = 0;
+  const unsigned seen = (x.there >> wave & 1) && k0 + (tid >> 2) < end ? 0xffffffffu : 0u;
+  auto odd = [](unsigned w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };   // halves whose exponent is all ones
+  x.vs &= seen;
+  unsigned any = odd(x.vs);
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const float f = g & 1 ? hi_bf16(x.ks[g / 2]) : lo_bf16(x.ks[g / 2]);
-    const bool finite = f - f == 0.f;
-    s.k[g] = seen && finite ? f : 0.f;
-    s.bad |= seen && !finite ? 256 : 0;
+  for (int i = 0; i < G / 2; ++i) {
+    x.ks[i] &= seen;
+    any |= odd(x.ks[i]);
   }
-  const float f = lo_bf16(x.vs);
-  const bool finite = f - f == 0.f;
-  s.v = seen && finite ? f : 0.f;
-  s.bad |= seen && !finite ? 1 << ((tid & 3) * G / 4) : 0;
-  return s;
+  int bad = 0;
+  if (__builtin_expect(__any(any != 0), 0)) {
+#pragma unroll
+    for (int i = 0; i < G / 2; ++i) {
+      const unsigned w = odd(x.ks[i]);
+      bad |= w ? 256 : 0;
+      x.ks[i] &= (w & 0x8000u ? 0u : 0xffffu) | (w >> 31 ? 0u : 0xffff0000u);
+    }
+    const bool v = odd(x.vs) != 0;
+    bad |= v ? 1 << ((tid & 3) * G / 4) : 0;
+    x.vs = v ? 0u : x.vs;
+  }
+  return bad;
 }
 // Half of word n (key words, then value words) of the piece: n = slot / 2.  `part` takes the first half to the second.
 template <int D>
-__device__ __forceinline__ void unpack_slot(const Stage<D>& x, lds_cptr keys, lds_cptr values, int slot, const Scales<D>& s, bf16x4& part) {
+__device__ __forceinline__ void unpack_slot(const Stage<D>& x, LDS_PTR(char) keys, LDS_PTR(char) values, int slot, bf16x4& part) {
   constexpr int G = D / 32;
   const int n = slot >> 1;
-  unsigned w = n >= G ? x.v[n - G] : x.k[n];
-  asm volatile("" : "+v"(w));                                // (here, not ahead of the products)
-  const bf16x4 y = unpack4(w, slot & 1, n >= G ? s.v : s.k[n]);
-  if (slot & 1)
-    *(LDS_PTR(bf16x8))(n >= G ? flip_bits(values, (n - G) << 4) : flip_bits(keys, n << 6)) = __builtin_shufflevector(part, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  const float s = n >= G ? lo_bf16(x.vs) : n & 1 ? hi_bf16(x.ks[n / 2]) : lo_bf16(x.ks[n / 2]);
+  const bf16x4 y = unpack4(n >= G ? x.v[n - G] : x.k[n], slot & 1, s);
+  if (slot & 1) *(LDS_PTR(bf16x8))(n >= G ? values + (n - G) * 16 : keys + n * 64) = __builtin_shufflevector(part, y, 0, 1, 2, 3, 4, 5, 6, 7);
   else part = y;
 }
 // What is not finite in the wave's chunk.
@@ -189,12 +192,12 @@ __device__ __forceinline__ void note_bad(LDS_PTR(char) lds, int buf, int bad) {
   }
 }
 template <int D>
-__device__ __forceinline__ void unpack_stage(const Stage<D>& x, LDS_PTR(char) lds, int buf, lds_cptr keys, lds_cptr values, int k0, int end) {
-  const Scales<D> s = piece_scales<D>(x, k0, end);
+__device__ __forceinline__ void unpack_stage(Stage<D>& x, LDS_PTR(char) lds, int buf, LDS_PTR(char) keys, LDS_PTR(char) values, int k0, int end) {
+  const int bad = clean_scales<D>(x, k0, end);
   bf16x4 part;
 #pragma unroll
-  for (int slot = 0; slot < D / 8; ++slot) unpack_slot<D>(x, keys, values, slot, s, part);
-  note_bad<D>(lds, buf, s.bad);
+  for (int slot = 0; slot < D / 8; ++slot) unpack_slot<D>(x, keys, values, slot, part);
+  note_bad<D>(lds, buf, bad);
 }
 
 // Fragment f, issued before at most N later LDS operations, has landed.
@@ -307,13 +310,15 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
       load_stage<D>(xa, a.c, piece, pb, e0, k_begin, k_end);
       load_stage<D>(xb, a.c, piece, pb, e1, k_begin + kKeys, k_end);
       __syncthreads();                                       // the buffers are free
-      unpack_stage<D>(xa, lds, 0, lds + unpack_keys_at<D>(), lds + unpack_values_at<D>(), k_begin, visible);
+      unpack_stage<D>(xa, lds, 0, lds + unpack_keys_at<D>(tid), lds + unpack_values_at<D>(tid), k_begin, visible);
       int there = xa.there;
       load_stage<D>(xa, a.c, piece, pb, e2, k_begin + 2 * kKeys, k_end);
       __syncthreads();
-      lds_cptr pk = lds_row_ptr<D>(lds, l32, 8 * half), pv0, pv1;   // this buffer's fragments; the other's unpacked pieces
-      lds_tr_ptrs<D>(lds + kTileBytes<D>, 0, lane, pv0, pv1);
-      lds_cptr uk = keep(lds + 2 * kTileBytes<D> + unpack_keys_at<D>()), uv = keep(lds + 2 * kTileBytes<D> + unpack_values_at<D>());
+      // this buffer's fragments, the other's unpacked pieces
+      lds_cptr pk = keep(lds + l32 * kKRow<D> + 16 * half);
+      lds_cptr pv = keep(lds + kKeys * kKRow<D> + (4 * (lane >> 5) + (lane >> 2 & 3)) * kVRow<D> + 32 * (lane >> 4 & 1) + 8 * (lane & 3));
+      LDS_PTR(char) uk = lds + kBuffer<D> + unpack_keys_at<D>(tid);
+      LDS_PTR(char) uv = lds + kBuffer<D> + unpack_values_at<D>(tid);
 
       // The products of tile k0 in buffer BUF, and between them the other work: x, the next tile, is unpacked beside the first half's scores and the
       // second half's O^T products; a half's probabilities are formed beside the products that follow its scores.  A half is 32 keys.  A
@@ -329,16 +334,14 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
         floatx16 sacc[2][2];                                 // [half][group]
         bf16x8 kf[NF];
         short4v vf[NV][2];
-        // (the second half's addresses from a copy: equal ones would be kept from the first)
-        const lds_cptr qk = keep(pk), qv0 = keep(pv0), qv1 = keep(pv1);
         auto issue = [&](auto o_) {
           constexpr int o = decltype(o_)::value;
           if constexpr (o < NF) {
-            r1_issue<(o / NKS) * 64 * D>(flip_bits(o < NKS ? pk : qk, (o % NKS) << 5), kf[o]);
+            r1_issue<(o / NKS) * 32 * kKRow<D> + (o % NKS) * 32>(pk, kf[o]);
           } else if constexpr (o < NF + NV) {
             constexpr int p = o - NF;
-            tr1_issue<(p / NDB) * 32 * D>(flip_bits(p < 2 * NDB ? pv0 : qv0, (p % NDB) << 6), vf[p][0]);
-            tr1_issue<(p / NDB) * 32 * D>(flip_bits(p < 2 * NDB ? pv1 : qv1, (p % NDB) << 6), vf[p][1]);
+            tr1_issue<(p / NDB) * 16 * kVRow<D> + (p % NDB) * 64>(pv, vf[p][0]);
+            tr1_issue<((p / NDB) * 16 + 8) * kVRow<D> + (p % NDB) * 64>(pv, vf[p][1]);
           }
         };
         constexpr auto later = [](int o) {                   // LDS reads issued behind fragment o's when it is used
@@ -366,7 +369,6 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
           constexpr int kb = decltype(kb_)::value;
           const bool moves = !(fmaxf(sum[0], sum[1]) <= kLazySum) || sum[0] != sum[0] || sum[1] != sum[1] || fminf(m[0], m[1]) == -INFINITY;
           if (__builtin_expect(__any(moves), 0)) {
-            const lds_cptr again = keep(pk);
             rest(oacc);
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
@@ -375,7 +377,7 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
               for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
               for (int ks = 0; ks < NKS; ++ks)
-                s = mfma32(*(LDS_PTR(const bf16x8))(flip_bits(again, ks << 5) + kb * 64 * D), qf[g][ks], s);
+                s = mfma32(*(LDS_PTR(const bf16x8))(pk + kb * 32 * kKRow<D> + ks * 32), qf[g][ks], s);
               if (masked) mask(s, kb, g);
               float mx = s[0];
 #pragma unroll
@@ -411,12 +413,13 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
               probability(kb_, e & 1, sacc[decltype(kb_)::value][e & 1], e >> 1);
             });
         };
-        const Scales<D> sc = piece_scales<D>(x, k0 + kKeys, visible);
+        const int bad = clean_scales<D>(x, k0 + kKeys, visible);
         bf16x4 part;
         static_for<0, kAhead>([&](auto o_) { issue(o_); });
         static_for<0, 2 * NKS>([&](auto i_) {
           constexpr int i = decltype(i_)::value, ks = i / 2, g = i % 2;
           if constexpr (g == 0) wait_frag<later(ks)>(kf[ks]);
+          if constexpr (g == 0) unpack_slot<D>(x, uk, uv, ks, part);
           if constexpr (ks == 0) {
             const floatx16 zero = {};
             sacc[0][g] = mfma32(kf[ks], qf[g][ks], zero);
@@ -424,7 +427,6 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
             sacc[0][g] = mfma32(kf[ks], qf[g][ks], sacc[0][g]);
           }
           if constexpr (g == 1) issue(IC<ks + kAhead>{});
-          else unpack_slot<D>(x, uk, uv, ks, sc, part);
           __builtin_amdgcn_sched_barrier(0);
         });
         if (masked) {
@@ -436,6 +438,7 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
         static_for<0, 2 * NKS>([&](auto i_) {
           constexpr int i = decltype(i_)::value, ks = i / 2, g = i % 2, o = NKS + ks;
           if constexpr (g == 0) wait_frag<later(o)>(kf[o]);
+          share(IC<0>{}, i_);
           if constexpr (ks == 0) {
             const floatx16 zero = {};
             sacc[1][g] = mfma32(kf[o], qf[g][ks], zero);
@@ -443,7 +446,6 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
             sacc[1][g] = mfma32(kf[o], qf[g][ks], sacc[1][g]);
           }
           if constexpr (g == 1) issue(IC<o + kAhead>{});
-          share(IC<0>{}, i_);
           __builtin_amdgcn_sched_barrier(0);
         });
         settle(IC<0>{});
@@ -455,9 +457,9 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
         static_for<0, 4 * NDB>([&](auto i_) {
           constexpr int i = decltype(i_)::value, p = i / 2, g = i % 2;
           if constexpr (g == 0) wait_frag<later(NF + p)>(vf[p][0], vf[p][1]);
+          share(IC<1>{}, i_);
           mfma_acc(oacc[g][p % NDB], join_frag(vf[p][0], vf[p][1]), weights(p / NDB, g));
           if constexpr (g == 1) issue(IC<NF + p + kAhead>{});
-          share(IC<1>{}, i_);
           __builtin_amdgcn_sched_barrier(0);
         });
         settle(IC<1>{});
@@ -467,12 +469,12 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
         static_for<0, 4 * NDB>([&](auto i_) {
           constexpr int i = decltype(i_)::value, p = 2 * NDB + i / 2, g = i % 2;
           if constexpr (g == 0) wait_frag<later(NF + p)>(vf[p][0], vf[p][1]);
+          if constexpr (g == 0) unpack_slot<D>(x, uk, uv, NKS + i / 2, part);
           mfma_acc(oacc[g][p % NDB], join_frag(vf[p][0], vf[p][1]), weights(p / NDB, g));
           if constexpr (g == 1) issue(IC<NF + p + kAhead>{});
-          else unpack_slot<D>(x, uk, uv, NKS + i / 2, sc, part);
           __builtin_amdgcn_sched_barrier(0);
         });
-        note_bad<D>(lds, BUF ^ 1, sc.bad);
+        note_bad<D>(lds, BUF ^ 1, bad);
         if (__builtin_amdgcn_readfirstlane(any_bad)) {       // scales that are not finite: NaN where their keys are seen
           rest(oacc);
 #pragma unroll
@@ -500,8 +502,8 @@ __global__ __launch_bounds__(kThreads, 1) void cache_attn_wide_kernel(AttnArgs a
         const int entry_now = entry;
         entry = load_entry(a.c, table, k0 + 4 * kKeys, k_end);   // (first: loads complete in order)
         load_stage<D>(x, a.c, piece, pb, entry_now, k0 + 3 * kKeys, k_end);
-        constexpr int to_other = BUF ? -2 * kTileBytes<D> : 2 * kTileBytes<D>;
-        pk += to_other; pv0 += to_other; pv1 += to_other;
+        constexpr int to_other = BUF ? -kBuffer<D> : kBuffer<D>;
+        pk += to_other; pv += to_other;
         uk -= to_other; uv -= to_other;
         // this tile's reads and the next one's writes are done (loads on their way may stay so)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
