@@ -14,7 +14,6 @@ SOURCES = ["builder.cpp", "solver.cpp", "dag.cpp", "search.cpp", "tables.cpp", "
 # builtin products of the same kernel must then be told to stay in architectural registers.
 EXTRA_FLAGS = {"dkdv_wide_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "fwd_wide_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "cache_attn_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                # pairs of products that the vectoriser forms and the target takes apart again keep the lane broadcasts out of them
                "cache_attn.hip": ["-fno-slp-vectorize"]}
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wno-unused-command-line-argument",

@@ -5,7 +5,6 @@
 
 namespace slimattn {
 
-constexpr int kThreads = 256, kWaves = 4;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaxGrid = 1024;       // at most four blocks per compute unit
 
@@ -51,7 +50,8 @@ __device__ __forceinline__ long long wave_scan(long long x) {   // inclusive
   return x;
 }
 
-// Inclusive scan over the block; `total` gets the sum.
+// Inclusive scan over the block of THREADS; `total` gets the sum.
+template <int THREADS>
 __device__ __forceinline__ long long block_scan(long long x, long long* lds, long long& total) {
   x = wave_scan(x);
   const int wave = threadIdx.x >> 6;
@@ -60,7 +60,7 @@ __device__ __forceinline__ long long block_scan(long long x, long long* lds, lon
   __syncthreads();
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     if (w < wave) x += lds[w];
     total += lds[w];
   }
@@ -78,18 +78,18 @@ struct Place {
 };
 
 // Row: what a sequence adds (units_of_all(), items()), and how many blocks share a row of so much work.  False: nothing to do for this block.
-// Up to 256 sequences are one look at the lengths.
-template <class Row>
+// As many sequences as the block has threads are one look at the lengths.
+template <class Row, int THREADS>
 __device__ __forceinline__ bool find_place(const AttnArgs& a, int N, int id, long long* scan, long long* found, Header* header, Place& p) {
   const int tid = threadIdx.x;
-  const bool one_look = a.c.n_seqs <= kThreads, with_items = Row::kNeedsItems || a.slots;
+  const bool one_look = a.c.n_seqs <= THREADS, with_items = Row::kNeedsItems || a.slots;
   long long mine = 0, my_items = 0, items = 0;
-  for (int b = tid; b < a.c.n_seqs; b += kThreads) {
+  for (int b = tid; b < a.c.n_seqs; b += THREADS) {
     const Row s(a, b);
     mine += s.units_of_all();
     my_items += s.items();
   }
-  const long long units_to = block_scan(mine, scan, p.total), items_to = with_items ? block_scan(my_items, scan, items) : 0;
+  const long long units_to = block_scan<THREADS>(mine, scan, p.total), items_to = with_items ? block_scan<THREADS>(my_items, scan, items) : 0;
   p.blocks = Row::blocks(a, N, p.total, items);
   if (blockIdx.x == 0 && tid == 0) header->listed = a.slots ? (int)min((long long)a.slots, items) : p.blocks;
   if (id >= p.blocks) return false;
@@ -99,7 +99,7 @@ __device__ __forceinline__ bool find_place(const AttnArgs& a, int N, int id, lon
     if (p.begin < units_to && p.begin >= units_to - mine) { found[0] = tid; found[1] = units_to - mine; found[2] = items_to - my_items; }
   } else {
     long long units_before = 0, items_before = 0;
-    for (int b0 = 0;; b0 += kThreads) {                      // ends: begin < total
+    for (int b0 = 0;; b0 += THREADS) {                      // ends: begin < total
       const int b = b0 + tid;
       long long w = 0, i = 0, units = 0, n = 0;
       if (b < a.c.n_seqs) {
@@ -107,7 +107,7 @@ __device__ __forceinline__ bool find_place(const AttnArgs& a, int N, int id, lon
         w = s.units_of_all();
         i = s.items();
       }
-      const long long end = units_before + block_scan(w, scan, units), item_end = with_items ? items_before + block_scan(i, scan, n) : 0;
+      const long long end = units_before + block_scan<THREADS>(w, scan, units), item_end = with_items ? items_before + block_scan<THREADS>(i, scan, n) : 0;
       if (p.begin < end && p.begin >= end - w) { found[0] = b; found[1] = end - w; found[2] = item_end - i; }
       if (p.begin < units_before + units) break;
       units_before += units;

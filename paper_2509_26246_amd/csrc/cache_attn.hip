@@ -23,6 +23,7 @@
 namespace slimattn {
 namespace {
 
+constexpr int kThreads = 256, kWaves = 4;
 constexpr int kCols = 16;            // query columns of a tile
 constexpr int kStep = 64;            // keys of a wave's step
 constexpr int kUnit = kWaves * kStep;
@@ -288,7 +289,7 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
   const int id = N % 8 == 0 ? (int)(blockIdx.x % 8) * (N / 8) + blockIdx.x / 8 : blockIdx.x;
 
   Place place;
-  if (!find_place<NarrowRow>(a, N, id, scan, found, split_header(ws), place)) return;
+  if (!find_place<NarrowRow, kThreads>(a, N, id, scan, found, split_header(ws), place)) return;
   const int n = place.blocks;
   const long long U = place.total, u0 = place.begin, u1 = place.end;
   int b = place.seq;
