@@ -372,3 +372,56 @@ def test_binding_refuses_what_is_not_a_matching_tensor():
     c.workspace = c.workspace[:64]
     with pytest.raises(ValueError):
         c.attend(q, torch.empty_like(q), lse, 0.1)
+
+
+def test_pages_that_are_not_there_for_many_query_columns():
+    hq, hkv, d, dt, n, rows = 16, 2, 128, torch.bfloat16, 200, 40            # 320 columns of a sequence
+    c = _cache([n, n], hkv, d, dt, 32, max_rows=2 * rows, hq=hq, extra=0)
+    k, v = _values((2 * n, hkv, d), 1, dt), _values((2 * n, hkv, d), 2, dt)
+    c.write(k.cuda(), v.cuda(), _ptr([n, n]))
+    c.page_table[0, 2], c.page_table[1, 0], c.page_table[1, 6] = -1, c._shape["n_pages"], 1 << 30
+    q = _values((2 * rows, hq, d), 3, dt, False)
+    o, lse = torch.empty(2 * rows, hq, d, dtype=dt, device="cuda"), torch.empty(hq, 2 * rows, device="cuda")
+    c.attend(q.cuda(), o, lse, 0.1, _ptr([rows, rows]))
+    kh, vh = R.held(k), R.held(v)
+    for b, gone in enumerate(((2,), (0, 6))):
+        for i in (0, 7, 30, 39):
+            keep = [b * n + j for j in range(n - rows + i + 1) if j // 32 not in gone]
+            at = b * rows + i
+            _check_attend(o[at:at + 1], lse[:, at:at + 1], q[at:at + 1], kh[keep], vh[keep], [len(keep)], [1], hq // 2, 0.1, dt)
+    c.page_table.fill_(-1)
+    c.attend(q.cuda(), o, lse, 0.1, _ptr([rows, rows]))
+    assert (o == 0).all() and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("scale,qf", [(0.0, 1.0), (-0.3, 1.0), (1e-30, 1.0), (0.1, 30.0)])
+def test_scales_for_many_query_columns(scale, qf):
+    _attend([300, 20, 257], [40, 20, 33], 16, 2, 64, "bf16", 16, scale=scale, qf=qf)
+
+
+def test_the_same_bits_for_many_query_columns_beside_few_and_in_a_graph():
+    lens, rows, hq, hkv, d = [5000, 300, 700], [200, 2, 90], 8, 2, 128
+    c, q, o, lse = _attend(lens, rows, hq, hkv, d, "bf16", 64)
+    q, ptr = q.cuda(), _ptr(rows)
+    g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    o2, lse2 = torch.zeros_like(o), torch.zeros_like(lse)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=side):
+        c.attend(q, o2, lse2, d ** -0.5, ptr)
+    for n in ([5000, 300, 700], [4000, 299, 60], [150, 1, 700], [5000, 300, 700]):
+        c.lens.copy_(torch.tensor(n))
+        c.workspace.fill_(0xFF)
+        c.attend(q, o, lse, d ** -0.5, ptr)
+        o2.zero_()
+        c.workspace.fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    # the rows dealt out otherwise; the later sequences now reach positions never written, whose NaN are equal only as bits
+    ptr.copy_(torch.tensor([0, 2, 202, 292]))
+    c.lens.copy_(torch.tensor([300, 700, 5000]))
+    c.attend(q, o, lse, d ** -0.5, ptr)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.isfinite(o[:2].float()).all()
+    assert torch.equal(o.view(torch.int16), o2.view(torch.int16)) and torch.equal(lse.view(torch.int32), lse2.view(torch.int32))
