@@ -103,6 +103,11 @@ def make_problem(q: np.ndarray, k: np.ndarray, v: np.ndarray, dO: np.ndarray, cu
                    torch.empty((T, hkv, d), dtype=tdt, device=device), ws)
 
 
+def _stream() -> int:
+    """The current stream's handle, without the object around it (2 us of a call that takes 10)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
 def _lib_dtype(dtype: torch.dtype) -> int:
     if dtype == torch.bfloat16:
         return B.BF16
@@ -134,7 +139,7 @@ class Rotary:
 
     def _kw(self, tokens: int):
         return dict(self._shape, total_tokens=tokens, q_weight=self.q_weight, k_weight=self.k_weight,
-                    stream=torch.cuda.current_stream().cuda_stream)
+                    stream=_stream())
 
     def forward(self, q, k, positions, q_out, k_out):
         """q, k [T, heads, d] (columns of a fused projection, or packed), positions int32 [axes, T] or [T] -> q_out, k_out, packed."""
@@ -165,7 +170,7 @@ class KVCache:
             self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=page_table.device)
 
     def _kw(self, n_rows: int):
-        return dict(self._shape, n_rows=n_rows, stream=torch.cuda.current_stream().cuda_stream)
+        return dict(self._shape, n_rows=n_rows, stream=_stream())
 
     def write(self, k, v, row_ptr=None):
         """k, v [rows, Hkv, d]: the last tokens of the sequences (row_ptr: first row of each; None: one each) into their pages."""
