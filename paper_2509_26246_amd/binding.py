@@ -510,8 +510,8 @@ def _torch_dtype(dtype):
 
 def _current_device() -> int:
     """Index of the current GPU; -2 (no tensor's) where the program has not used one."""
-    cuda = _torch().cuda
-    return cuda.current_device() if cuda.is_initialized() else -2
+    torch = _torch()
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
 
 
 def _tensor_ptr(t, dtype, numel: int, what: str, dev: int):
