@@ -2,11 +2,13 @@
 //
 // Mathematics.  Of 32 channels, a = max |x|; scale s = a / 6 rounded to six significant bits (ties to even); code = the nearest of the 4-bit
 // floats to x / s, ties to the even code.  Both roundings are those of the real quotients: a / 6 is a correctly rounded 32-bit quotient, and
-// so is x / s here (product with 1 / s, one exact remainder, one correction).  A correctly rounded quotient is at a border only if the
-// real one is: borders have at most 7 bits and s six, so a 24-bit x off the border is off by more than half a step of the quotient.
+// so is x / s here (product with 1 / s, one exact remainder, one correction).  A correctly rounded quotient is at a border between two codes only if the
+// real one is: borders have three bits and s six, so border * s is itself a 24-bit number; an x beside it is off by a whole step, and its quotient by more than
+// half a step of the border's.
 //
 // Bound by memory and latency: 2 bytes in, 0.56 out for a bf16 value (and back).  A lane takes eight channels (16 bytes of bf16, one word of codes), four lanes
-// share a scale by two lane exchanges; a wave stays with one row, whose page it looks up once.
+// share a scale by two lane exchanges; a wave stays with one row, whose page it looks up once.  Measured, bf16, 8 heads of 128: 10764 rows (57 MB either
+// way) 12.7 us written, 11.0 read (4.5 and 5.1 TB/s); 21188 rows read 20.9 us (5.3 TB/s); 64 rows 3.0 and 2.8 us, a launch's latency.
 #include <hip/hip_runtime.h>
 
 #include "cache.h"

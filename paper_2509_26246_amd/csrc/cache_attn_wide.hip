@@ -6,10 +6,11 @@
 // columns (a lane holds one column's scores, so sums and maxima need one lane exchange), tiles are double-buffered, and the next tile's codes are loaded
 // a tile ahead of that and unpacked beside the products of this one.  LDS rows are padded, so that a fragment is one address and a constant.
 //
-// 1024 new rows behind 31K keys, 32 heads over 8, head dim 128 (135 GFLOP): 168 us in all, 800 TFLOP/s; the narrow kernel takes 293 us.  No single part
-// binds it: without the exponentials, the second product, the unpacking or the loads (each taken out alone) 5 to 8% go.  Four waves of 32 columns,
-// two blocks to a compute unit, and four waves of 64 columns came within 4% of it; with eight waves a tile is unpacked for the most columns and every
-// register file holds two waves, whose products and softmax run beside each other.
+// 1024 new rows behind 31K keys, 8 heads over one, head dim 128 (135 GFLOP): 157 us in all, 860 TFLOP/s; the narrow kernel takes 293 us.  A tile of 64 keys
+// takes a compute unit 2 us (1050 TFLOP/s; a large library product reaches 1220), the rest is fixed: finding the work, first loads, parts, join.  No
+// single part binds a tile: matrix unit 43% of the cycles, vector unit 50%, LDS 45%; without the exponentials, the second product, the unpacking
+// or the loads (each taken out alone) 5 to 8% go.  Within 4% of it came four waves of 32 columns, two blocks to a compute unit, and four waves of 64
+// columns; within 1% four buffers with a barrier every second tile, V rows padded for half the reads' conflicts, and wave priorities.
 //
 // Work.  A tile's columns see the keys up to their last row, so the tiles of one prompt differ in length: a tile weighs (keys before the rows + a fixed
 // part) * group + its last column's number, which adds up to a closed form over tiles; weights are divided evenly among the blocks, cuts fall on
