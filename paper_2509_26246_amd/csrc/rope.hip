@@ -328,7 +328,7 @@ RopeArgs make_args(const slimattn_rope_params& p) {
   a.dq_stride = p.dq_stride ? p.dq_stride : (long long)p.n_q_heads * d;
   a.dk_stride = p.dk_stride ? p.dk_stride : (long long)p.n_kv_heads * d;
   int left[4] = {0, 0, 0, 0}, axis = 0;
-  for (int i = 0; i < p.n_axes; ++i) left[i] = p.sections[i];
+  for (int i = 0; p.rotary_dim > 0 && i < p.n_axes; ++i) left[i] = p.sections[i];   // (n_axes is checked where there is a rotation)
   for (int i = 0; i < p.rotary_dim / 2; ++i) {             // sections add up to the number of pairs
     while (left[axis] == 0) axis = (axis + 1) & 3;
     --left[axis];

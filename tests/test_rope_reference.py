@@ -93,3 +93,9 @@ def test_workspace_is_the_same_for_any_number_of_tokens():
     need = {S.rope_bwd_workspace_bytes(t, **shape) for t in (0, 1, 7, 4096, 1 << 20)}
     assert len(need) == 1 and need.pop() > 0
     assert S.rope_bwd_workspace_bytes(64, **dict(shape, flags=0)) == 0 and S.rope_bwd_workspace_bytes(64, **dict(shape, head_dim=48)) == 0
+
+
+@pytest.mark.parametrize("n", [5, 400])
+def test_axes_are_not_looked_at_without_a_rotation(n):
+    shape = dict(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=S.BF16, rotary_dim=0, sections=[0] * n, flags=S.ROPE_NORM)
+    S.rope_bwd(None, None, None, None, None, None, None, None, None, None, None, total_tokens=0, **shape)
