@@ -548,6 +548,8 @@ def _rows_ptr(t, T: int, heads: int, d: int, dtype, stride: int, what: str, dev:
     s = t.stride()
     if s[2] != 1 or (heads > 1 and s[1] != d):
         raise ValueError(f"{what}: the heads of a token must lie one behind the other")
+    if T > 1 and s[0] < heads * d:                              # (0 would be taken for packed rows)
+        raise ValueError(f"{what}: the rows of an expanded or overlapping tensor are not rows of its memory")
     return t.data_ptr(), s[0] if T > 1 else 0
 
 

@@ -97,3 +97,14 @@ def test_sizes():
     assert S.cache_bytes(0, 16, 2, 64) == 0 and S.cache_bytes(8, 24, 2, 64) == 0 and S.cache_bytes(1 << 20, 256, 8, 128) == (1 << 20) * 256 * 8 * 144
     assert S.cache_attn_workspace_bytes(8, **GOOD) > 0
     assert S.cache_attn_workspace_bytes(7, **GOOD) == 0 and S.cache_attn_workspace_bytes(8, **dict(GOOD, head_dim=32)) == 0
+
+
+def test_expanded_rows_are_refused(monkeypatch):
+    from paper_2509_26246_amd import binding as B
+    monkeypatch.setattr(B, "_current_device", lambda: -1)      # (tensors of the CPU pass for the GPU's: every call is refused before a launch)
+    k = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
+    lens, table, cache = torch.zeros(4, dtype=torch.int32), torch.zeros(4, 4, dtype=torch.int32), torch.zeros(8 * 16 * 2 * 72, dtype=torch.uint8)
+    for bad in (k[:1].expand(4, 2, 64), k[:, :1].expand(4, 2, 64)):
+        for pair in ((bad, k), (k, bad)):
+            with pytest.raises(ValueError):
+                S.cache_write(*pair, cache, table, lens, **GOOD)

@@ -99,3 +99,15 @@ def test_workspace_is_the_same_for_any_number_of_tokens():
 def test_axes_are_not_looked_at_without_a_rotation(n):
     shape = dict(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=S.BF16, rotary_dim=0, sections=[0] * n, flags=S.ROPE_NORM)
     S.rope_bwd(None, None, None, None, None, None, None, None, None, None, None, total_tokens=0, **shape)
+
+
+def test_expanded_and_overlapping_rows_are_refused(monkeypatch):
+    from paper_2509_26246_amd import binding as B
+    monkeypatch.setattr(B, "_current_device", lambda: -1)      # (tensors of the CPU pass for the GPU's: every call is refused before a launch)
+    q, k = torch.zeros(8, 4, 64, dtype=torch.bfloat16), torch.zeros(8, 2, 64, dtype=torch.bfloat16)
+    pos, freq, outs = torch.zeros(8, dtype=torch.int32), torch.ones(32), [torch.zeros_like(q), torch.zeros_like(k)]
+    for bad in (q[:1].expand(8, 4, 64), q.flatten().as_strided((8, 4, 64), (64, 64, 1)), q[:, :1].expand(8, 4, 64)):
+        with pytest.raises(ValueError):
+            S.rope_fwd(bad, k, pos, freq, *outs, **GOOD)
+        with pytest.raises(ValueError):
+            S.rope_bwd(q, k, pos, freq, *outs, bad, k, None, None, None, **GOOD)
