@@ -405,7 +405,7 @@ int slimattn_bwd_static(const slimattn_params* p, const void* q, const void* k, 
 #define SLIMATTN_ROPE_DEALT     4   /* pairs are dealt to the axes in turn; otherwise each axis has a block of neighbouring pairs */
 
 typedef struct slimattn_rope_params {
-  int32_t total_tokens;           /* T */
+  int32_t total_tokens;           /* T, 0 .. 2^27 */
   int32_t n_q_heads, n_kv_heads;  /* Hq, Hkv >= 0, not both 0 (0: no queries or no keys; their pointers are not looked at) */
   int32_t head_dim;               /* d: 16, 32, 64 or 128 */
   int32_t dtype;                  /* SLIMATTN_F32 or SLIMATTN_BF16: the tensors; weights are float, arithmetic is fp32 */
@@ -458,8 +458,8 @@ typedef struct slimattn_cache_params {
   int32_t n_kv_heads, head_dim;   /* Hkv; d: 64 or 128 */
   int32_t dtype;                  /* SLIMATTN_F32 or SLIMATTN_BF16: k, v, q, o */
   int32_t n_seqs;                 /* sequences, 0 .. 65536 */
-  int32_t max_pages;              /* columns of the page table, >= 1; max_pages * page_size < 2^31 */
-  int32_t n_rows;                 /* rows of k, v, q, o */
+  int32_t max_pages;              /* columns of the page table, >= 1; max_pages * page_size <= 2^30 */
+  int32_t n_rows;                 /* rows of k, v, q, o: 0 .. 2^25 */
 } slimattn_cache_params;
 
 /* The calls below share these DEVICE int32 arrays, which they read when they run (a recorded call follows what the arrays then hold):

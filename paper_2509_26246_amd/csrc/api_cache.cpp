@@ -30,8 +30,9 @@ bool geometry_ok(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t
 int check(const slimattn_cache_params* p) {
   if (!p || (p->dtype != SLIMATTN_F32 && p->dtype != SLIMATTN_BF16)) return SLIMATTN_EINVAL;
   if (!geometry_ok(p->n_pages, p->page_size, p->n_kv_heads, p->head_dim)) return SLIMATTN_EINVAL;
-  if (p->n_seqs < 0 || p->n_seqs > 65536 || p->max_pages < 1 || p->n_rows < 0) return SLIMATTN_EINVAL;
-  if ((int64_t)p->max_pages * p->page_size > INT32_MAX) return SLIMATTN_EINVAL;
+  if (p->n_seqs < 0 || p->n_seqs > 65536 || p->max_pages < 1) return SLIMATTN_EINVAL;
+  if (p->n_rows < 0 || p->n_rows > (1 << 25)) return SLIMATTN_EINVAL;            // a wave a row, 2^32 threads a launch; strides times rows in 64 bits
+  if ((int64_t)p->max_pages * p->page_size > (1 << 30)) return SLIMATTN_EINVAL;   // positions and the steps behind them in 32 bits
   return SLIMATTN_OK;
 }
 

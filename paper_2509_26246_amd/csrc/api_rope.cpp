@@ -42,7 +42,8 @@ int check(const slimattn_rope_params* p) {
   if (!p || (p->dtype != SLIMATTN_F32 && p->dtype != SLIMATTN_BF16)) return SLIMATTN_EINVAL;
   const int d = p->head_dim;
   if (d != 16 && d != 32 && d != 64 && d != 128) return SLIMATTN_EINVAL;
-  if (p->total_tokens < 0 || p->n_q_heads < 0 || p->n_kv_heads < 0 || p->n_q_heads + (int64_t)p->n_kv_heads < 1) return SLIMATTN_EINVAL;
+  if (p->total_tokens < 0 || p->total_tokens > (1 << 27)) return SLIMATTN_EINVAL;   // 16 threads a token, 2^32 a launch; strides times tokens in 64 bits
+  if (p->n_q_heads < 0 || p->n_kv_heads < 0 || p->n_q_heads + (int64_t)p->n_kv_heads < 1) return SLIMATTN_EINVAL;
   if (p->n_q_heads > 65535 || p->n_kv_heads > 65535) return SLIMATTN_EINVAL;
   if (p->flags & ~(SLIMATTN_ROPE_NORM | SLIMATTN_ROPE_ADJACENT | SLIMATTN_ROPE_DEALT)) return SLIMATTN_EINVAL;
   const bool norm = p->flags & SLIMATTN_ROPE_NORM;

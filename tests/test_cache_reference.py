@@ -108,3 +108,12 @@ def test_expanded_rows_are_refused(monkeypatch):
         for pair in ((bad, k), (k, bad)):
             with pytest.raises(ValueError):
                 S.cache_write(*pair, cache, table, lens, **GOOD)
+
+
+@pytest.mark.parametrize("call", ["write", "read", "attn"])
+@pytest.mark.parametrize("bad", [dict(n_rows=(1 << 25) + 1, row_ptr=16), dict(max_pages=(1 << 26) + 1)], ids=str)
+def test_sizes_beyond_a_launch_and_beyond_positions_are_refused(call, bad):
+    far = dict(k=1 << 44, v=1 << 45, q=1 << 46, o=1 << 47)
+    with pytest.raises(S.SlimAttnError) as e:
+        _call(call, dict(far, **bad))
+    assert e.value.code == -1

@@ -111,3 +111,9 @@ def test_expanded_and_overlapping_rows_are_refused(monkeypatch):
             S.rope_fwd(bad, k, pos, freq, *outs, **GOOD)
         with pytest.raises(ValueError):
             S.rope_bwd(q, k, pos, freq, *outs, bad, k, None, None, None, **GOOD)
+
+
+def test_more_tokens_than_a_launch_has_threads_for_are_refused():
+    far = dict(total_tokens=(1 << 27) + 1, n_q_heads=1, n_kv_heads=0)
+    _refused("fwd", **far, k=0, k_out=0, q=1 << 40, q_out=1 << 42)
+    _refused("bwd", **far, k=0, k_out=0, q=1 << 40, q_out=1 << 42, dq=1 << 44)
