@@ -428,6 +428,7 @@ typedef struct slimattn_rope_params {
  * q [T, Hq, d] by q_stride, k [T, Hkv, d] by k_stride -> q_out, k_out packed, as slimattn_fwd reads them.  q_weight, k_weight float [d]
  * (SLIMATTN_ROPE_NORM; NULL: ones); positions int32 [n_axes, T]; inv_freq float [rotary_dim / 2].  All DEVICE; tensors 16-byte
  * aligned, the rest 4-byte.  q_out may be q (k_out be k) where that is packed; other overlaps of an output are refused.
+ * A row whose sum of squares is beyond fp32 (or an infinity or a NaN in it) is NaN with SLIMATTN_ROPE_NORM, in all its channels.
  * Allocates nothing, does not synchronise, one kernel launch. */
 int slimattn_rope_fwd(const slimattn_rope_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,
                       const int32_t* positions, const float* inv_freq, void* q_out, void* k_out, void* stream);
@@ -462,7 +463,8 @@ typedef struct slimattn_cache_params {
   int32_t n_rows;                 /* rows of k, v, q, o: 0 .. 2^25 */
 } slimattn_cache_params;
 
-/* The calls below share these DEVICE int32 arrays, which they read when they run (a recorded call follows what the arrays then hold):
+/* The calls below share these DEVICE int32 arrays, which they read when they run (a recorded call follows what the arrays then hold, and they
+ * must not change while one runs):
  *   lens [n_seqs]                   tokens of each sequence, the rows of this call included;
  *   row_ptr [n_seqs + 1] or NULL    rows row_ptr[b] .. row_ptr[b+1] - 1 of the tensors are the last tokens of sequence b, in order: of its
  *                                   n rows the i-th stands at position lens[b] - n + i.  Ascending.  NULL: one row each (n_rows = n_seqs);

@@ -99,7 +99,7 @@ __device__ __forceinline__ bool find_place(const AttnArgs& a, int N, int id, lon
     if (p.begin < units_to && p.begin >= units_to - mine) { found[0] = tid; found[1] = units_to - mine; found[2] = items_to - my_items; }
   } else {
     long long units_before = 0, items_before = 0;
-    for (int b0 = 0;; b0 += THREADS) {                      // ends: begin < total
+    for (int b0 = 0; b0 < a.c.n_seqs; b0 += THREADS) {       // (begin < total: some sequence has it)
       const int b = b0 + tid;
       long long w = 0, i = 0, units = 0, n = 0;
       if (b < a.c.n_seqs) {

@@ -120,7 +120,8 @@ def _lib_dtype(dtype: torch.dtype) -> int:
 
 class Rotary:
     """Norm per head and rotation of a layer's queries and keys, in front of slimattn_fwd, and their gradients behind slimattn_bwd: the
-    parameters of the layer and what its backward pass needs (workspace, weight gradients), for calls of any number of tokens."""
+    parameters of the layer and what its backward pass needs (workspace, weight gradients), for calls of any number of tokens.
+    One backward call at a time where it has a norm (its workspace, `dq_weight`, `dk_weight`)."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, inv_freq: Optional[torch.Tensor], *,
                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, norm: bool = False, eps: float = 1e-6,
@@ -155,7 +156,8 @@ class Rotary:
 
 class KVCache:
     """One layer's keys and values of a batch of sequences in 4 bits: the pages, the page table and the lengths (device tensors the program
-    updates as sequences grow), and the workspace of attention calls of up to `max_rows` rows."""
+    updates as sequences grow), and the workspace of attention calls of up to `max_rows` rows (and of one row a sequence).  One attention
+    call at a time: two streams, or two recorded graphs that may run together, need a handle each (`cache` may be shared)."""
 
     def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, page_table: torch.Tensor,
                  lens: torch.Tensor, *, max_rows: int = 0, n_q_heads: int = 0):
@@ -168,7 +170,7 @@ class KVCache:
         self.cache = torch.empty(size, dtype=torch.uint8, device=page_table.device)
         self.workspace = None
         if n_q_heads:
-            need = B.cache_attn_workspace_bytes(n_q_heads, n_rows=max_rows, **self._shape)
+            need = B.cache_attn_workspace_bytes(n_q_heads, n_rows=max(max_rows, page_table.shape[0]), **self._shape)
             self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=page_table.device)
 
     def _kw(self, n_rows: int):

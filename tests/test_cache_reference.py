@@ -117,3 +117,11 @@ def test_sizes_beyond_a_launch_and_beyond_positions_are_refused(call, bad):
     with pytest.raises(S.SlimAttnError) as e:
         _call(call, dict(far, **bad))
     assert e.value.code == -1
+
+
+def test_workspaces_grow_with_rows():
+    for dtype in (S.BF16, S.F32):
+        for hq, hkv, n_seqs, max_pages in ((8, 1, 1, 4), (8, 8, 64, 16), (64, 1, 3, 1000), (32, 8, 256, 64)):
+            shape = dict(n_pages=8, page_size=64, n_kv_heads=hkv, head_dim=128, dtype=dtype, n_seqs=n_seqs, max_pages=max_pages)
+            sizes = [S.cache_attn_workspace_bytes(hq, n_rows=n, **shape) for n in (0, 1, 2, 3, 16, 17, 100, 129, 1000, 5000, 100000)]
+            assert sizes == sorted(sizes) and sizes[0] > 0

@@ -425,3 +425,14 @@ def test_the_same_bits_for_many_query_columns_beside_few_and_in_a_graph():
     torch.cuda.synchronize()
     assert torch.isfinite(o[:2].float()).all()
     assert torch.equal(o.view(torch.int16), o2.view(torch.int16)) and torch.equal(lse.view(torch.int32), lse2.view(torch.int32))
+
+
+def test_a_handle_for_single_tokens_needs_no_row_count():
+    lens, d = [900, 3, 40], 64
+    c = _cache(lens, 2, d, torch.bfloat16, 16, hq=8)       # (max_rows = 0)
+    k, v = _values((sum(lens), 2, d), 1, torch.bfloat16), _values((sum(lens), 2, d), 2, torch.bfloat16)
+    c.write(k.cuda(), v.cuda(), _ptr(lens))
+    q = _values((3, 8, d), 3, torch.bfloat16, False)
+    o = torch.empty(3, 8, d, dtype=torch.bfloat16, device="cuda")
+    c.attend(q.cuda(), o, None, 0.125)
+    _check_attend(o, None, q, R.held(k), R.held(v), lens, [1, 1, 1], 4, 0.125, torch.bfloat16)
