@@ -436,3 +436,26 @@ def test_a_handle_for_single_tokens_needs_no_row_count():
     o = torch.empty(3, 8, d, dtype=torch.bfloat16, device="cuda")
     c.attend(q.cuda(), o, None, 0.125)
     _check_attend(o, None, q, R.held(k), R.held(v), lens, [1, 1, 1], 4, 0.125, torch.bfloat16)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_pages_behind_four_gigabytes(rows):
+    hq, hkv, d, page, lens, dt = 32, 8, 128, 64, [200, 131], torch.bfloat16
+    n_pages = (9 << 29) // (page * hkv * 144)                # 4.8 GB
+    c = _cache(lens, hkv, d, dt, page, max_rows=2 * rows, hq=hq, extra=n_pages)
+    n_pages = c._shape["n_pages"]
+    assert n_pages * page * hkv * 144 > 1 << 32
+    table = torch.full_like(c.page_table, 0x7fffffff)
+    table[0, :4] = torch.tensor([n_pages - 1, 3, n_pages // 2, n_pages - 2])
+    table[1, :3] = torch.tensor([n_pages - 4, 0, n_pages - 3])
+    c.page_table.copy_(table)
+    k, v = _values((sum(lens), hkv, d), 1, dt), _values((sum(lens), hkv, d), 2, dt)
+    c.write(k.cuda(), v.cuda(), _ptr(lens))
+    kk, vv = torch.empty_like(k, device="cuda"), torch.empty_like(k, device="cuda")
+    c.read(kk, vv, _ptr(lens))
+    _same(kk, R.held(k))
+    _same(vv, R.held(v))
+    q = _values((2 * rows, hq, d), 3, dt, False)
+    o, lse = torch.empty(2 * rows, hq, d, dtype=dt, device="cuda"), torch.empty(hq, 2 * rows, device="cuda")
+    c.attend(q.cuda(), o, lse, d ** -0.5, _ptr([rows, rows]))
+    _check_attend(o, lse, q, R.held(k), R.held(v), lens, [rows, rows], hq // hkv, d ** -0.5, dt)

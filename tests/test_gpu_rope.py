@@ -223,3 +223,22 @@ def test_binding_refuses_what_is_not_a_matching_tensor():
             rot.forward(*bad)
     with pytest.raises(S.SlimAttnError):
         rot.forward(q, k, pos, torch.empty(T * 2 * d + 1, device="cuda")[1:], o(k))   # not 16-byte aligned
+
+
+def test_elements_behind_two_to_the_31():
+    T, hq, hkv, d, dt = (1 << 18) + 5, 64, 2, 128, torch.bfloat16
+    freq = torch.tensor([1e4 ** (-2 * i / d) for i in range(d // 2)], dtype=torch.float32).cuda()
+    rot = H.Rotary(hq, hkv, d, dt, freq, norm=True)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k = (torch.randn(T, h, d, generator=g, device="cuda", dtype=dt) for h in (hq, hkv))
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    assert q.numel() > 1 << 31
+    n = 300
+    last = [t[-n:].clone() for t in (q, k)]
+    want, outs = [torch.empty_like(t) for t in last], [torch.empty_like(q), torch.empty_like(k)]
+    rot.forward(*last, pos[-n:].contiguous(), *want)
+    rot.forward(q, k, pos, *outs)
+    assert all(torch.equal(a[-n:], b) for a, b in zip(outs, want))
+    rot.backward(*last, pos[-n:].contiguous(), *[t[-n:].contiguous() for t in outs], *want)
+    rot.backward(q, k, pos, *outs, q, k)                     # (in place of the inputs)
+    assert torch.equal(q[-n:], want[0]) and torch.equal(k[-n:], want[1])
