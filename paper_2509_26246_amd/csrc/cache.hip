@@ -33,15 +33,16 @@ template <> __device__ __forceinline__ void load8<float>(const float* p, float (
 #pragma unroll
   for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
 }
+// Rows read back are streamed past the caches: 21188 rows of 8 heads of 128 30.0 -> 21.0 us among other work; slimattn_fwd behind it within 0.5%.
 __device__ __forceinline__ void store8(bf16* p, const float (&x)[8]) {
   bf16x8 v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (bf16)x[i];
-  *reinterpret_cast<bf16x8*>(p) = v;
+  __builtin_nontemporal_store(v, reinterpret_cast<bf16x8*>(p));
 }
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  *reinterpret_cast<floatx4*>(p) = floatx4{x[0], x[1], x[2], x[3]};
-  *reinterpret_cast<floatx4*>(p + 4) = floatx4{x[4], x[5], x[6], x[7]};
+  __builtin_nontemporal_store(floatx4{x[0], x[1], x[2], x[3]}, reinterpret_cast<floatx4*>(p));
+  __builtin_nontemporal_store(floatx4{x[4], x[5], x[6], x[7]}, reinterpret_cast<floatx4*>(p + 4));
 }
 
 // The scale of 32 channels from the largest |x| (its bits: infinities and NaN are the largest).  Below 2^-100 a group is zero (its
