@@ -495,7 +495,7 @@ size_t slimattn_cache_attn_workspace_bytes(const slimattn_cache_params* p, int32
 /* Attention of the rows over their sequences' caches: the row at position p sees keys 0 .. p,
  * S_j = scale * q . k_j, lse = log sum_j exp S_j, o = sum_j exp(S_j - lse) v_j.  q, o [n_rows, Hq, d] packed, Hq a multiple of Hkv (query head h
  * uses KV head h / (Hq / Hkv)); lse float [Hq, n_rows] or NULL; o must not overlap q.  The keys of long sequences are divided among blocks
- * and the parts added in their order: the same call on the same inputs gives the same bits.  Sequences of more than 128 query columns (rows x Hq / Hkv) take a kernel of their own in
+ * and the parts added in their order: the same call on the same inputs gives the same bits.  Sequences of more than 112 query columns (rows x Hq / Hkv) take a kernel of their own in
  * bf16, which only runs where n_rows allows for such a sequence: one, two or four launches.  An infinity or a NaN in a group of 32 channels
  * makes NaN of the rows that see its key (of a value: in those channels), and of no others. */
 int slimattn_cache_attn(const slimattn_cache_params* p, int32_t n_q_heads, float scale, const void* q, const int32_t* row_ptr,

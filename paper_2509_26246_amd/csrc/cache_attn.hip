@@ -538,10 +538,11 @@ int launch_cache_attn_wide(const slimattn_cache_params& p, int n_q_heads, AttnAr
 namespace {
 
 // Which kernel takes a sequence goes by its number of query columns, which the device knows (row_ptr): the narrow kernel's time grows with the
-// tiles of 16, the wide one's steps up every 256.  d 128, 32 heads over 8, us narrow / wide at 64, 128, 192, 256, 512 columns: one sequence of 32K keys 39 / 60,
-// 61 / 61, 79 / 64, 92 / 66, 159 / 98; eight of 4K 42 / 60, 63 / 63, 67 / 67, 103 / 71, 178 / 108; 32 of 1K 53 / 55, 76 / 57, 80 / 60, 121 / 64, 212 / 109.  Where there is little to do
-// (8K keys, two heads) the wide kernel's larger parts cost more than it saves, up to 512 columns: 21 / 32, 35 / 38.
-constexpr long long kNarrowCols = 128;
+// tiles of 16, the wide one's steps up every 256.  d 128, 32 heads over 8, us narrow / wide at 64, 96, 128 columns a sequence, caches in rotation: 16 of 4K keys
+// 69 / 91, 71 / 92, 109 / 93; 64 of 4K 218 / 283, 264 / 305, 384 / 293; 128 of 1K 137 / 168, 170 / 172, 233 / 177; at 64, 128, 256, 512 columns, one cache: one sequence of
+// 32K keys 39 / 60, 61 / 61, 92 / 66, 159 / 98; eight of 4K 42 / 60, 63 / 63, 103 / 71, 178 / 108.  Where there is little to do (8K keys, two heads) the
+// wide kernel's larger parts cost more than it saves, up to 512 columns: 21 / 32, 35 / 38.
+constexpr long long kNarrowCols = 112;
 bool may_be_wide(const slimattn_cache_params& p, int n_q_heads, bool ragged) {
   return p.dtype == SLIMATTN_BF16 && (ragged ? p.n_rows : 1ll) * (n_q_heads / p.n_kv_heads) > kNarrowCols;
 }
