@@ -8,7 +8,7 @@
 //
 // Bound by memory and latency: 2 bytes in, 0.56 out for a bf16 value (and back).  A lane takes eight channels (16 bytes of bf16, one word of codes), four lanes
 // share a scale by two lane exchanges; a wave stays with one row, whose page it looks up once.  Measured, bf16, 8 heads of 128: 10764 rows (57 MB either
-// way) 12.7 us written, 11.0 read (4.5 and 5.1 TB/s); 21188 rows read 20.9 us (5.3 TB/s); 64 rows 3.0 and 2.8 us, a launch's latency.
+// way) 13.3 us written, 11.8 read (4.3 and 4.8 TB/s); 21188 rows read 20.0 us (5.6 TB/s); 64 rows 3.0 us, a launch's latency.
 #include <hip/hip_runtime.h>
 
 #include "cache.h"

@@ -12,7 +12,7 @@
 // the blocks of one launch, which find their place in that row by a scan over the lengths (they are data: a recorded call follows
 // them).  A block's first and last item may be parts; parts leave O, maximum and sum in the workspace, and a second launch adds them up in the
 // order of the keys (done by the same launch, its last blocks would have to wait for the others' parts behind counters that something has to clear).
-// Measured, bf16, d 128: 64 sequences of up to 4096 keys, 32 heads over 8 (195 MB) 42 us and 5 for the joins, 4.6 TB/s; four of up to 131072 keys, 8 heads over one
+// Measured, bf16, d 128: 64 sequences of up to 4096 keys, 32 heads over 8 (195 MB) 43 us and 5 for the joins, 4.6 TB/s; four of up to 131072 keys, 8 heads over one
 // (75 MB) 20 and 6 us, of which 4 and 2.5 are launch and latency; one of 876 keys 7.4 and 3: a chain of lengths, page, cache and parts.  A unit is 4 waves x 64 keys; each wave keeps its own state and shares nothing before the end of an item.
 //
 // A wave's step, 64 keys (lane group h = lane / 16 holds keys 16h .. 16h+15 of everything): the next step's codes and scales are loaded while

@@ -7,8 +7,8 @@
 // Bound by memory: the forward reads and writes each element once, the backward reads x and dy and writes dx.  So that a pass needs no
 // exchange but the sum of squares, a lane holds two runs of four channels that contain both halves of its four pairs, whichever way
 // pairs are formed: channels 4j .. 4j+3 and rotary/2 + 4j .. (8 j .. 8j+7 where neighbours pair up, or behind the rotated channels).
-// Measured: 32768 tokens of 32 + 8 heads of 128, bf16: forward 129 us (0.67 GB, 5.2 TB/s; a large copy reaches 4.9), backward 215 us (1.0 GB, 4.7 TB/s) and 3 to 5
-// for the weights' sums; 4099 tokens of 8 + 2 heads, fp32: 11 and 13 us; 16 tokens of 32 + 8 heads, forward: 4.3 us, launch and one walk's latency.
+// Measured: 32768 tokens of 32 + 8 heads of 128, bf16: forward 129 us (0.67 GB, 5.2 TB/s; a large copy reaches 4.9), backward 213 us (1.0 GB, 4.7 TB/s) and 3 to 5
+// for the weights' sums; 4099 tokens of 8 + 2 heads, fp32: 10 and 13 us; 16 tokens of 32 + 8 heads, forward: 4.2 us, launch and one walk's latency.
 // A head takes d/8 lanes, a wave 64 / (d/8) heads; the lanes of one head ("group") keep a token and walk its heads, so the four
 // sines and cosines of a lane are computed once per token and not once per head.  Few tokens are divided by heads as well.
 //
