@@ -554,14 +554,15 @@ def _rows_ptr(t, T: int, heads: int, d: int, dtype, stride: int, what: str, dev:
 
 
 def _raise(rc: int, where: str) -> None:
-    if rc != 0:
-        raise SlimAttnError(rc, where, f" hip={load_library().slimattn_last_hip_error()}" if rc == -4 else "")
+    raise SlimAttnError(rc, where, f" hip={load_library().slimattn_last_hip_error()}" if rc == -4 else "")
 
 
-# Parameter structures are kept by their plain values: a program calls with few of them, and filling one costs as much as a launch.
+# Parameter structures are kept by their plain values: a program calls with few of them, and filling one costs as much as a launch.  `shape` below is
+# what stays the same from call to call, in the structures' order; the functions that take it are those behind the handles of harness.py.
 @lru_cache(maxsize=512)
-def _rope_params(T, hq, hkv, d, dtype, rotary_dim, sections, eps, flags, q_stride=0, k_stride=0, dq_stride=0, dk_stride=0):
+def _rope_params(T, shape, q_stride=0, k_stride=0, dq_stride=0, dk_stride=0):
     """(structure, its workspace bytes)."""
+    hq, hkv, d, dtype, rotary_dim, sections, eps, flags = shape
     p = _RopeParams(total_tokens=T, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, dtype=dtype, rotary_dim=rotary_dim, n_axes=len(sections),
                     eps=eps, flags=flags, q_stride=q_stride, k_stride=k_stride, dq_stride=dq_stride, dk_stride=dk_stride)
     if len(sections) <= 4:                                      # (the library refuses more axes)
@@ -569,26 +570,51 @@ def _rope_params(T, hq, hkv, d, dtype, rotary_dim, sections, eps, flags, q_strid
     return p, int(load_library().slimattn_rope_bwd_workspace_bytes(C.byref(p)))
 
 
+def _rope_fwd(dev, stream, T, shape, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out, q_stride=0, k_stride=0):
+    hq, hkv, d, dtype, rotary_dim, sections = shape[:6]
+    td, f32 = _torch_dtype(dtype), _torch_dtype(F32)
+    pq, q_stride = _rows_ptr(q, T, hq, d, td, q_stride, "q", dev)
+    pk, k_stride = _rows_ptr(k, T, hkv, d, td, k_stride, "k", dev)
+    rc = (_lib or load_library()).slimattn_rope_fwd(
+        _rope_params(T, shape, q_stride, k_stride)[0], pq, pk, _tensor_ptr(q_weight, f32, d, "q_weight", dev), _tensor_ptr(k_weight, f32, d, "k_weight", dev),
+        _tensor_ptr(positions, _torch_dtype("int32"), len(sections) * T, "positions", dev), _tensor_ptr(inv_freq, f32, rotary_dim // 2, "inv_freq", dev),
+        _tensor_ptr(q_out, td, T * d * hq, "q_out", dev), _tensor_ptr(k_out, td, T * d * hkv, "k_out", dev), stream)
+    if rc != 0:
+        _raise(rc, "slimattn_rope_fwd")
+
+
 def rope_fwd(q, k, positions, inv_freq, q_out, k_out, *, total_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int,
              rotary_dim: int, sections: Sequence[int], q_weight=None, k_weight=None, eps: float = 1e-6, flags: int = 0, q_stride: int = 0,
              k_stride: int = 0, stream: Optional[int] = None) -> None:
     """slimattn_rope_fwd: q, k [T, heads, d] (rows any distance apart, for raw addresses q_stride, k_stride) -> q_out, k_out packed."""
-    lib = _lib or load_library()
-    T, d, td, f32, dev = total_tokens, head_dim, _torch_dtype(dtype), _torch_dtype(F32), _current_device()
-    pq, q_stride = _rows_ptr(q, T, n_q_heads, d, td, q_stride, "q", dev)
-    pk, k_stride = _rows_ptr(k, T, n_kv_heads, d, td, k_stride, "k", dev)
-    sections = tuple(sections)
-    p, _ = _rope_params(T, n_q_heads, n_kv_heads, d, dtype, rotary_dim, sections, eps, flags, q_stride, k_stride)
-    rc = lib.slimattn_rope_fwd(p, pq, pk, _tensor_ptr(q_weight, f32, d, "q_weight", dev), _tensor_ptr(k_weight, f32, d, "k_weight", dev),
-                               _tensor_ptr(positions, _torch_dtype("int32"), len(sections) * T, "positions", dev),
-                               _tensor_ptr(inv_freq, f32, rotary_dim // 2, "inv_freq", dev), _tensor_ptr(q_out, td, T * d * n_q_heads, "q_out", dev),
-                               _tensor_ptr(k_out, td, T * d * n_kv_heads, "k_out", dev), stream)
-    _raise(rc, "slimattn_rope_fwd")
+    _rope_fwd(_current_device(), stream, total_tokens, (n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, tuple(sections), eps, flags), q, k, positions,
+              inv_freq, q_weight, k_weight, q_out, k_out, q_stride, k_stride)
 
 
 def rope_bwd_workspace_bytes(total_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, rotary_dim: int,
                              sections: Sequence[int], eps: float = 1e-6, flags: int = 0) -> int:
-    return _rope_params(total_tokens, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, tuple(sections), eps, flags)[1]
+    return _rope_params(total_tokens, (n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, tuple(sections), eps, flags))[1]
+
+
+def _rope_bwd(dev, stream, T, shape, q, k, positions, inv_freq, q_weight, k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, q_stride=0,
+              k_stride=0, dq_stride=0, dk_stride=0):
+    hq, hkv, d, dtype, rotary_dim, sections = shape[:6]
+    td, f32 = _torch_dtype(dtype), _torch_dtype(F32)
+    pq, q_stride = _rows_ptr(q, T, hq, d, td, q_stride, "q", dev)
+    pk, k_stride = _rows_ptr(k, T, hkv, d, td, k_stride, "k", dev)
+    pdq, dq_stride = _rows_ptr(dq, T, hq, d, td, dq_stride, "dq", dev)
+    pdk, dk_stride = _rows_ptr(dk, T, hkv, d, td, dk_stride, "dk", dev)
+    p, need = _rope_params(T, shape, q_stride, k_stride, dq_stride, dk_stride)
+    if dq_weight is None and dk_weight is None:
+        need = 0
+    rc = (_lib or load_library()).slimattn_rope_bwd(
+        p, pq, pk, _tensor_ptr(q_weight, f32, d, "q_weight", dev), _tensor_ptr(k_weight, f32, d, "k_weight", dev),
+        _tensor_ptr(positions, _torch_dtype("int32"), len(sections) * T, "positions", dev), _tensor_ptr(inv_freq, f32, rotary_dim // 2, "inv_freq", dev),
+        _tensor_ptr(dq_out, td, T * d * hq, "dq_out", dev), _tensor_ptr(dk_out, td, T * d * hkv, "dk_out", dev), pdq, pdk,
+        _tensor_ptr(dq_weight, f32, d, "dq_weight", dev), _tensor_ptr(dk_weight, f32, d, "dk_weight", dev),
+        _tensor_ptr(workspace, _torch_dtype("uint8"), need, "workspace", dev), stream)
+    if rc != 0:
+        _raise(rc, "slimattn_rope_bwd")
 
 
 def rope_bwd(q, k, positions, inv_freq, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, *, total_tokens: int, n_q_heads: int,
@@ -596,35 +622,19 @@ def rope_bwd(q, k, positions, inv_freq, dq_out, dk_out, dq, dk, dq_weight, dk_we
              eps: float = 1e-6, flags: int = 0, q_stride: int = 0, k_stride: int = 0, dq_stride: int = 0, dk_stride: int = 0,
              stream: Optional[int] = None) -> None:
     """slimattn_rope_bwd: dq_out, dk_out packed -> dq, dk (rows any distance apart) and, with ROPE_NORM, dq_weight, dk_weight."""
-    lib = _lib or load_library()
-    T, d, td, f32, dev = total_tokens, head_dim, _torch_dtype(dtype), _torch_dtype(F32), _current_device()
-    pq, q_stride = _rows_ptr(q, T, n_q_heads, d, td, q_stride, "q", dev)
-    pk, k_stride = _rows_ptr(k, T, n_kv_heads, d, td, k_stride, "k", dev)
-    pdq, dq_stride = _rows_ptr(dq, T, n_q_heads, d, td, dq_stride, "dq", dev)
-    pdk, dk_stride = _rows_ptr(dk, T, n_kv_heads, d, td, dk_stride, "dk", dev)
-    sections = tuple(sections)
-    p, need = _rope_params(T, n_q_heads, n_kv_heads, d, dtype, rotary_dim, sections, eps, flags, q_stride, k_stride, dq_stride, dk_stride)
-    if dq_weight is None and dk_weight is None:
-        need = 0
-    rc = lib.slimattn_rope_bwd(p, pq, pk, _tensor_ptr(q_weight, f32, d, "q_weight", dev), _tensor_ptr(k_weight, f32, d, "k_weight", dev),
-                               _tensor_ptr(positions, _torch_dtype("int32"), len(sections) * T, "positions", dev),
-                               _tensor_ptr(inv_freq, f32, rotary_dim // 2, "inv_freq", dev), _tensor_ptr(dq_out, td, T * d * n_q_heads, "dq_out", dev),
-                               _tensor_ptr(dk_out, td, T * d * n_kv_heads, "dk_out", dev), pdq, pdk, _tensor_ptr(dq_weight, f32, d, "dq_weight", dev),
-                               _tensor_ptr(dk_weight, f32, d, "dk_weight", dev), _tensor_ptr(workspace, _torch_dtype("uint8"), need, "workspace", dev),
-                               stream)
-    _raise(rc, "slimattn_rope_bwd")
+    _rope_bwd(_current_device(), stream, total_tokens, (n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, tuple(sections), eps, flags), q, k, positions,
+              inv_freq, q_weight, k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, q_stride, k_stride, dq_stride, dk_stride)
 
 
 @lru_cache(maxsize=512)
-def _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows):
+def _cache_params(shape, n_rows):
     """(structure, bytes of the cache)."""
-    return (_CacheParams(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows),
-            cache_bytes(n_pages, page_size, n_kv_heads, head_dim))
+    return _CacheParams(*shape, n_rows), cache_bytes(*shape[:4])
 
 
 @lru_cache(maxsize=512)
-def _cache_attn_bytes(n_q_heads, *shape):
-    return int(load_library().slimattn_cache_attn_workspace_bytes(_cache_params(*shape)[0], n_q_heads))
+def _cache_attn_bytes(n_q_heads, shape, n_rows):
+    return int(load_library().slimattn_cache_attn_workspace_bytes(_cache_params(shape, n_rows)[0], n_q_heads))
 
 
 def cache_bytes(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int) -> int:
@@ -639,44 +649,59 @@ def _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev):
             _tensor_ptr(page_table, i32, p.n_seqs * p.max_pages, "page_table", dev), _tensor_ptr(cache, _torch_dtype("uint8"), size, "cache", dev))
 
 
+def _cache_write(dev, stream, n_rows, shape, k, v, cache, page_table, lens, row_ptr, k_stride=0, v_stride=0):
+    hkv, d, td = shape[2], shape[3], _torch_dtype(shape[4])
+    p, size = _cache_params(shape, n_rows)
+    pk, k_stride = _rows_ptr(k, n_rows, hkv, d, td, k_stride, "k", dev)
+    pv, v_stride = _rows_ptr(v, n_rows, hkv, d, td, v_stride, "v", dev)
+    rc = (_lib or load_library()).slimattn_cache_write(p, pk, pv, k_stride, v_stride, *_cache_arrays(p, size, cache, page_table, lens, row_ptr, dev), stream)
+    if rc != 0:
+        _raise(rc, "slimattn_cache_write")
+
+
 def cache_write(k, v, cache, page_table, lens, row_ptr=None, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
                 dtype: int, n_seqs: int, max_pages: int, k_stride: int = 0, v_stride: int = 0, stream: Optional[int] = None) -> None:
     """slimattn_cache_write: k, v [n_rows, Hkv, d] (rows any distance apart, for raw addresses k_stride, v_stride) into the cache."""
-    lib, td, dev = _lib or load_library(), _torch_dtype(dtype), _current_device()
-    p, size = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
-    pk, k_stride = _rows_ptr(k, n_rows, n_kv_heads, head_dim, td, k_stride, "k", dev)
-    pv, v_stride = _rows_ptr(v, n_rows, n_kv_heads, head_dim, td, v_stride, "v", dev)
+    _cache_write(_current_device(), stream, n_rows, (n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages), k, v, cache, page_table, lens,
+                 row_ptr, k_stride, v_stride)
+
+
+def _cache_read(dev, stream, n_rows, shape, cache, page_table, lens, row_ptr, k, v):
+    td, n = _torch_dtype(shape[4]), n_rows * shape[2] * shape[3]
+    p, size = _cache_params(shape, n_rows)
     rp, ln, pt, ca = _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev)
-    _raise(lib.slimattn_cache_write(p, pk, pv, k_stride, v_stride, rp, ln, pt, ca, stream), "slimattn_cache_write")
+    rc = (_lib or load_library()).slimattn_cache_read(p, ca, rp, ln, pt, _tensor_ptr(k, td, n, "k", dev), _tensor_ptr(v, td, n, "v", dev), stream)
+    if rc != 0:
+        _raise(rc, "slimattn_cache_read")
 
 
 def cache_read(cache, page_table, lens, k, v, row_ptr=None, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
                dtype: int, n_seqs: int, max_pages: int, stream: Optional[int] = None) -> None:
     """slimattn_cache_read: the cache's values of the rows -> k, v [n_rows, Hkv, d] packed."""
-    lib, td, dev = _lib or load_library(), _torch_dtype(dtype), _current_device()
-    p, size = _cache_params(n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
-    rp, ln, pt, ca = _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev)
-    n = n_rows * n_kv_heads * head_dim
-    _raise(lib.slimattn_cache_read(p, ca, rp, ln, pt, _tensor_ptr(k, td, n, "k", dev), _tensor_ptr(v, td, n, "v", dev), stream), "slimattn_cache_read")
+    _cache_read(_current_device(), stream, n_rows, (n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages), cache, page_table, lens, row_ptr, k, v)
 
 
 def cache_attn_workspace_bytes(n_q_heads: int, *, n_rows: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: int,
                                n_seqs: int, max_pages: int) -> int:
-    return _cache_attn_bytes(n_q_heads, n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
+    return _cache_attn_bytes(n_q_heads, (n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages), n_rows)
+
+
+def _cache_attn(dev, stream, n_rows, shape, n_q_heads, scale, q, cache, page_table, lens, row_ptr, o, lse, workspace):
+    td, n = _torch_dtype(shape[4]), n_rows * n_q_heads * shape[3]
+    p, size = _cache_params(shape, n_rows)
+    rc = (_lib or load_library()).slimattn_cache_attn(
+        p, n_q_heads, scale, _tensor_ptr(q, td, n, "q", dev), *_cache_arrays(p, size, cache, page_table, lens, row_ptr, dev), _tensor_ptr(o, td, n, "o", dev),
+        _tensor_ptr(lse, _torch_dtype(F32), n_rows * n_q_heads, "lse", dev),
+        _tensor_ptr(workspace, _torch_dtype("uint8"), _cache_attn_bytes(n_q_heads, shape, n_rows), "workspace", dev), stream)
+    if rc != 0:
+        _raise(rc, "slimattn_cache_attn")
 
 
 def cache_attn(q, cache, page_table, lens, o, lse, workspace, row_ptr=None, *, n_q_heads: int, scale: float, n_rows: int, n_pages: int,
                page_size: int, n_kv_heads: int, head_dim: int, dtype: int, n_seqs: int, max_pages: int, stream: Optional[int] = None) -> None:
     """slimattn_cache_attn: q [n_rows, Hq, d] over the cache -> o, and lse [Hq, n_rows] unless it is None."""
-    lib, td, dev = _lib or load_library(), _torch_dtype(dtype), _current_device()
-    shape = (n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages, n_rows)
-    p, size = _cache_params(*shape)
-    rp, ln, pt, ca = _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev)
-    n = n_rows * n_q_heads * head_dim
-    rc = lib.slimattn_cache_attn(p, n_q_heads, scale, _tensor_ptr(q, td, n, "q", dev), rp, ln, pt, ca, _tensor_ptr(o, td, n, "o", dev),
-                                 _tensor_ptr(lse, _torch_dtype(F32), n_rows * n_q_heads, "lse", dev),
-                                 _tensor_ptr(workspace, _torch_dtype("uint8"), _cache_attn_bytes(n_q_heads, *shape), "workspace", dev), stream)
-    _raise(rc, "slimattn_cache_attn")
+    _cache_attn(_current_device(), stream, n_rows, (n_pages, page_size, n_kv_heads, head_dim, dtype, n_seqs, max_pages), n_q_heads, scale, q, cache, page_table,
+                lens, row_ptr, o, lse, workspace)
 
 
 STATIC_SCRATCH_BYTES = 64 << 20

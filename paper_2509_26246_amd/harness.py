@@ -103,11 +103,12 @@ def make_problem(q: np.ndarray, k: np.ndarray, v: np.ndarray, dO: np.ndarray, cu
                    torch.empty((T, hkv, d), dtype=tdt, device=device), ws)
 
 
-def _stream() -> int:
-    """The current stream's handle, without the object around it (3 us of a call that took 11)."""
+def _here():
+    """Index of the current GPU and handle of its current stream, without the object around it (3 us of a call that took 11)."""
     if not torch.cuda.is_initialized():
         torch.cuda.init()
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    dev = torch._C._cuda_getDevice()
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
 
 
 def _lib_dtype(dtype: torch.dtype) -> int:
@@ -130,28 +131,23 @@ class Rotary:
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         self.inv_freq, self.q_weight, self.k_weight, self.norm = inv_freq, q_weight, k_weight, norm
         rotary_dim = head_dim if rotary_dim is None else rotary_dim
-        self._shape = dict(n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=_lib_dtype(dtype), rotary_dim=rotary_dim,
-                           sections=tuple(sections) if sections is not None else (rotary_dim // 2,), eps=eps,
-                           flags=B.ROPE_NORM * norm | B.ROPE_ADJACENT * adjacent | B.ROPE_DEALT * dealt)
+        self._shape = (n_q_heads, n_kv_heads, head_dim, _lib_dtype(dtype), rotary_dim, tuple(sections) if sections is not None else (rotary_dim // 2,),
+                       eps, B.ROPE_NORM * norm | B.ROPE_ADJACENT * adjacent | B.ROPE_DEALT * dealt)
         self.dq_weight = self.dk_weight = self.workspace = None
         if norm:
-            need = B.rope_bwd_workspace_bytes(0, **self._shape)
+            need = B.rope_bwd_workspace_bytes(0, *self._shape)
             self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
             self.dq_weight = torch.zeros(head_dim, dtype=torch.float32, device=device)
             self.dk_weight = torch.zeros(head_dim, dtype=torch.float32, device=device)
 
-    def _kw(self, tokens: int):
-        return dict(self._shape, total_tokens=tokens, q_weight=self.q_weight, k_weight=self.k_weight,
-                    stream=_stream())
-
     def forward(self, q, k, positions, q_out, k_out):
         """q, k [T, heads, d] (columns of a fused projection, or packed), positions int32 [axes, T] or [T] -> q_out, k_out, packed."""
-        B.rope_fwd(q, k, positions, self.inv_freq, q_out, k_out, **self._kw((q if q is not None else k).shape[0]))
+        B._rope_fwd(*_here(), (q if q is not None else k).shape[0], self._shape, q, k, positions, self.inv_freq, self.q_weight, self.k_weight, q_out, k_out)
 
     def backward(self, q, k, positions, dq_out, dk_out, dq, dk):
         """dQ, dK of the attention and the forward's inputs -> dq, dk; the weights' gradients go to dq_weight, dk_weight."""
-        B.rope_bwd(q, k, positions, self.inv_freq, dq_out, dk_out, dq, dk, self.dq_weight, self.dk_weight, self.workspace,
-                   **self._kw((dq_out if dq_out is not None else dk_out).shape[0]))
+        B._rope_bwd(*_here(), (dq_out if dq_out is not None else dk_out).shape[0], self._shape, q, k, positions, self.inv_freq, self.q_weight,
+                    self.k_weight, dq_out, dk_out, dq, dk, self.dq_weight, self.dk_weight, self.workspace)
 
 
 class KVCache:
@@ -164,6 +160,7 @@ class KVCache:
         self.page_table, self.lens, self.n_q_heads = page_table, lens, n_q_heads
         self._shape = dict(n_pages=n_pages, page_size=page_size, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=_lib_dtype(dtype),
                            n_seqs=page_table.shape[0], max_pages=page_table.shape[1])
+        self._values = tuple(self._shape.values())
         size = B.cache_bytes(n_pages, page_size, n_kv_heads, head_dim)
         if size == 0:
             raise ValueError("cache: unsupported pages or heads")
@@ -173,18 +170,14 @@ class KVCache:
             need = B.cache_attn_workspace_bytes(n_q_heads, n_rows=max(max_rows, page_table.shape[0]), **self._shape)
             self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=page_table.device)
 
-    def _kw(self, n_rows: int):
-        return dict(self._shape, n_rows=n_rows, stream=_stream())
-
     def write(self, k, v, row_ptr=None):
         """k, v [rows, Hkv, d]: the last tokens of the sequences (row_ptr: first row of each; None: one each) into their pages."""
-        B.cache_write(k, v, self.cache, self.page_table, self.lens, row_ptr, **self._kw(k.shape[0]))
+        B._cache_write(*_here(), k.shape[0], self._values, k, v, self.cache, self.page_table, self.lens, row_ptr)
 
     def read(self, k, v, row_ptr=None):
         """The last tokens of the sequences from their pages -> k, v."""
-        B.cache_read(self.cache, self.page_table, self.lens, k, v, row_ptr, **self._kw(k.shape[0]))
+        B._cache_read(*_here(), k.shape[0], self._values, self.cache, self.page_table, self.lens, row_ptr, k, v)
 
     def attend(self, q, o, lse, scale, row_ptr=None):
         """q [rows, Hq, d], the queries of the sequences' last tokens, over their pages -> o, lse [Hq, rows] (or None)."""
-        B.cache_attn(q, self.cache, self.page_table, self.lens, o, lse, self.workspace, row_ptr, n_q_heads=self.n_q_heads, scale=scale,
-                     **self._kw(q.shape[0]))
+        B._cache_attn(*_here(), q.shape[0], self._values, self.n_q_heads, scale, q, self.cache, self.page_table, self.lens, row_ptr, o, lse, self.workspace)
