@@ -460,13 +460,15 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(AttnArgs a, T* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws) {
   constexpr int W = D / 4, R = kThreads / W;                 // threads of a row of D channels; runs
   const int tid = threadIdx.x;
-  if ((int)blockIdx.x >= split_header(ws)->listed) return;
-  const Split s = split_list(split_header(ws))[blockIdx.x];
-  if (s.parts == 0) return;
+  const Split s = split_list(split_header(ws))[blockIdx.x];  // (with the count, not behind it: the list has room for every block)
+  if ((int)blockIdx.x >= split_header(ws)->listed || s.parts == 0) return;
   __shared__ float weight[kMaxGrid], red[2 * kWaves];
   __shared__ float sums[R][D + 4];
   auto part = [&](int p) { return part_of<D>(ws, s.first + p, p == 0 ? 1 : 0); };
+  const int run = tid / W, e = (tid % W) * 4;
   for (int c = blockIdx.y; c < s.cols; c += gridDim.y) {
+    floatx4v x = {0.f, 0.f, 0.f, 0.f};
+    if (run < s.parts) x = *reinterpret_cast<const floatx4v*>(part(run) + c * D + e);   // on its way beside the statistics
     float m = -INFINITY, ms[kMaxGrid / kThreads], ls[kMaxGrid / kThreads];
 #pragma unroll
     for (int i = 0; i < kMaxGrid / kThreads; ++i) {
@@ -494,10 +496,9 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(AttnArgs a, T
     if ((tid & 63) == 0) red[kWaves + (tid >> 6)] = l;
     __syncthreads();
     l = (red[kWaves] + red[kWaves + 1]) + (red[kWaves + 2] + red[kWaves + 3]);
-    const int run = tid / W, e = (tid % W) * 4;
-    floatx4v x = {0.f, 0.f, 0.f, 0.f};
+    if (run < s.parts) x *= weight[run];
 #pragma unroll 4
-    for (int p = run; p < s.parts; p += R) x += *reinterpret_cast<const floatx4v*>(part(p) + c * D + e) * weight[p];
+    for (int p = run + R; p < s.parts; p += R) x += *reinterpret_cast<const floatx4v*>(part(p) + c * D + e) * weight[p];
     *reinterpret_cast<floatx4v*>(&sums[run][e]) = x;
     __syncthreads();
     if (run == 0) {

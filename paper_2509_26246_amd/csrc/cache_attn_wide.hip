@@ -510,11 +510,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a
 template <int D, int RUNS>
 __global__ __launch_bounds__(256) void cache_attn_wide_join_kernel(AttnArgs a, bf16* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws, size_t parts_at) {
   Header* header = split_header(ws + kListBytes);
-  if ((int)blockIdx.x >= header->listed) return;
-  const Split s = split_list(header)[blockIdx.x];
+  const Split s = split_list(header)[blockIdx.x];            // (with the count, not behind it: the list has room for every block)
   const int wave = blockIdx.y / (D / 32), db = blockIdx.y % (D / 32), r4 = RUNS == 1 ? threadIdx.x >> 6 : blockIdx.z, run = RUNS == 1 ? 0 : threadIdx.x >> 6;
   const int lane = threadIdx.x & 63, c = wave * 32 + (lane & 31);
-  if (s.parts == 0 || wave * 32 >= s.cols) return;
+  if ((int)blockIdx.x >= header->listed || s.parts == 0 || wave * 32 >= s.cols) return;
   const int each = (s.parts + RUNS - 1) / RUNS, begin = min(run * each, s.parts), end = min(begin + each, s.parts);
   auto part = [&](int p) { return part_of<D>(ws + parts_at, s.first + p, p == 0 ? 1 : 0); };
   float m = -INFINITY;
