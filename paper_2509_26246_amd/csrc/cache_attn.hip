@@ -456,23 +456,23 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
 
 // Adds up the parts of the split item listed at blockIdx.x, columns blockIdx.y, + gridDim.y, ...: runs of parts (thread / (D/4)) of four channels each,
 // in a fixed order.
-template <class T, int D>
-__global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(AttnArgs a, T* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws) {
-  constexpr int W = D / 4, R = kThreads / W;                 // threads of a row of D channels; runs
+template <class T, int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void cache_attn_join_kernel(AttnArgs a, T* __restrict__ o, float* __restrict__ lse, char* __restrict__ ws) {
+  constexpr int W = D / 4, R = THREADS / W, WAVES = THREADS / 64;                 // threads of a row of D channels; runs
   const int tid = threadIdx.x;
   const Split s = split_list(split_header(ws))[blockIdx.x];  // (with the count, not behind it: the list has room for every block)
   if ((int)blockIdx.x >= split_header(ws)->listed || s.parts == 0) return;
-  __shared__ float weight[kMaxGrid], red[2 * kWaves];
+  __shared__ float weight[kMaxGrid], red[2 * WAVES];
   __shared__ float sums[R][D + 4];
   auto part = [&](int p) { return part_of<D>(ws, s.first + p, p == 0 ? 1 : 0); };
   const int run = tid / W, e = (tid % W) * 4;
   for (int c = blockIdx.y; c < s.cols; c += gridDim.y) {
     floatx4v x = {0.f, 0.f, 0.f, 0.f};
     if (run < s.parts) x = *reinterpret_cast<const floatx4v*>(part(run) + c * D + e);   // on its way beside the statistics
-    float m = -INFINITY, ms[kMaxGrid / kThreads], ls[kMaxGrid / kThreads];
+    float m = -INFINITY, ms[kMaxGrid / THREADS], ls[kMaxGrid / THREADS];
 #pragma unroll
-    for (int i = 0; i < kMaxGrid / kThreads; ++i) {
-      const int p = tid + i * kThreads;
+    for (int i = 0; i < kMaxGrid / THREADS; ++i) {
+      const int p = tid + i * THREADS;
       ms[i] = p < s.parts ? part(p)[kCols * D + c] : -INFINITY;
       ls[i] = p < s.parts ? part(p)[kCols * D + kCols + c] : 0.f;
       m = fmaxf(m, ms[i]);
@@ -481,21 +481,25 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(AttnArgs a, T
     for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
     if ((tid & 63) == 0) red[tid >> 6] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    m = red[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, red[w]);
     const float ref = m == -INFINITY ? 0.f : m;
     float l = 0.f;
 #pragma unroll
-    for (int i = 0; i < kMaxGrid / kThreads; ++i) {
-      const int p = tid + i * kThreads;
+    for (int i = 0; i < kMaxGrid / THREADS; ++i) {
+      const int p = tid + i * THREADS;
       const float f = __builtin_amdgcn_exp2f(ms[i] - ref);
       if (p < s.parts) weight[p] = f;
       l = __builtin_fmaf(ls[i], f, l);
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
-    if ((tid & 63) == 0) red[kWaves + (tid >> 6)] = l;
+    if ((tid & 63) == 0) red[WAVES + (tid >> 6)] = l;
     __syncthreads();
-    l = (red[kWaves] + red[kWaves + 1]) + (red[kWaves + 2] + red[kWaves + 3]);
+    l = red[WAVES];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) l += red[WAVES + w];
     if (run < s.parts) x *= weight[run];
 #pragma unroll 4
     for (int p = run + R; p < s.parts; p += R) x += *reinterpret_cast<const floatx4v*>(part(p) + c * D + e) * weight[p];
@@ -577,6 +581,8 @@ int launch_cache_attn(const slimattn_cache_params& p, int n_q_heads, float scale
   const long long items = most_items(p, n_q_heads);
   a.slots = items < blocks ? (int)items : 0;
   const dim3 join(a.slots ? a.slots : blocks, a.slots && a.slots <= 64 ? kCols : 4);
+  // 32 parts of an item or more: 1024 threads, so that each adds up a few (four items of 131072 keys 27.1 -> 26.6 us in all; fewer parts gain nothing).
+  const bool many = a.slots && blocks >= 32 * a.slots;
   // Where sequences have 16 columns or fewer on average, their keys are read by one tile each and by nobody before the next call, with the other
   // layers' caches in between: streamed.  Caches in rotation, d 128, 32 heads over 8, us without / with: 19 MB 18.4 / 17.3, 76 MB 27.4 / 25.4, 303 MB
   // 76.9 / 65.9, 606 MB 133 / 115; 64 columns a sequence (four tiles) 222 / 229; a single cache read again and again from the last-level
@@ -593,7 +599,8 @@ int launch_cache_attn(const slimattn_cache_params& p, int n_q_heads, float scale
     else first(IC<0>{});
     const int e = (int)hipGetLastError();
     if (e != 0 || blocks < 2) return e;                      // one block holds every item whole
-    hipLaunchKernelGGL((cache_attn_join_kernel<T, D>), join, dim3(kThreads), 0, (hipStream_t)stream, a, (T*)o, lse, (char*)ws);
+    if (many) hipLaunchKernelGGL((cache_attn_join_kernel<T, D, 1024>), join, dim3(1024), 0, (hipStream_t)stream, a, (T*)o, lse, (char*)ws);
+    else hipLaunchKernelGGL((cache_attn_join_kernel<T, D, 256>), join, dim3(256), 0, (hipStream_t)stream, a, (T*)o, lse, (char*)ws);
     return (int)hipGetLastError();
   };
   if (p.dtype == SLIMATTN_F32) return p.head_dim == 128 ? run(float{}, IC<128>{}) : run(float{}, IC<64>{});
