@@ -190,27 +190,34 @@ __device__ __forceinline__ void score_step(float (&s)[16], const StepData<D>& x,
   });
 }
 
-// Scores of keys that a column does not see.  limit: the column's position (its last visible key); there: step_pages.
+// The lane's last visible key of a step, less what its lane group adds to a key's number.  limit: the column's position (its last visible key).
+__device__ __forceinline__ int last_of_step(int k0, int limit) { return limit - k0 - 4 * (int)((threadIdx.x & 63) >> 4); }
+// Whether the column sees the lane's key number e.  there: step_pages.
+__device__ __forceinline__ bool sees(int e, int last, unsigned there) { return 16 * (e >> 2) + (e & 3) <= last && (there >> (e >> 2) & 1); }
+
+// Scores of keys that a column does not see.
 __device__ __forceinline__ void mask_step(float (&s)[16], int k0, int limit, unsigned there) {
-  const int last = limit - k0 - 4 * (int)((threadIdx.x & 63) >> 4);
+  const int last = last_of_step(k0, limit);
 #pragma unroll
   for (int e = 0; e < 16; ++e)
-    if (16 * (e >> 2) + (e & 3) > last || !(there >> (e >> 2) & 1)) s[e] = -INFINITY;
+    if (!sees(e, last, there)) s[e] = -INFINITY;
 }
 
 // A masked step's value scales may be anything (keys behind the end) or rightly NaN for some columns only.  Products with a probability of 0
-// must not see them: scales that are not finite become 0, and columns that do see the key get their NaN here.
+// must not see them: scales that are not finite become 0, and columns that do see the key get their NaN here (whatever its probability came to: one
+// that is seen may have underflowed).
 template <int D>
-__device__ __forceinline__ void clean_scales(State<D>& st, const float (&s)[16], float (&vs)[D / 32]) {
+__device__ __forceinline__ void clean_scales(State<D>& st, float (&vs)[D / 32], int k0, int limit, unsigned there) {
   static_for<0, D / 32>([&](auto g_) {
     constexpr int g = decltype(g_)::value;
     const bool bad = !(vs[g] - vs[g] == 0.f);
     if (__any(bad)) {
       bool hit = false;
+      const int last = last_of_step(k0, limit);
       static_for<0, 16>([&](auto e_) {
         constexpr int e = decltype(e_)::value;
         const float f = from_lane<e>(vs[g]);
-        hit |= !(f - f == 0.f) && s[e] != 0.f;
+        hit |= !(f - f == 0.f) && sees(e, last, there);
       });
       hit |= (bool)__shfl_xor((int)hit, 16);                 // the column's other lane groups hold other channels
       hit |= (bool)__shfl_xor((int)hit, 32);
@@ -250,7 +257,7 @@ __device__ __forceinline__ void softmax_step(State<D>& st, float (&s)[16], float
     s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale_log2, -m));
     st.l += s[e];
   }
-  if (masked) clean_scales<D>(st, s, vs);
+  if (masked) clean_scales<D>(st, vs, k0, limit, there);
   static_for<0, G>([&](auto g_) {
     constexpr int g = decltype(g_)::value;
     float p[2][8];

@@ -1,0 +1,41 @@
+"""slimattn_cache_attn where its parts meet: values that are not finite under weights of zero, in every kind of step and in both kernels.
+
+A spoilt value's group of 32 channels has to be NaN in each row that sees its key, however small the key's weight is, and in no other row; tolerances of
+what is not spoilt are those of test_gpu_cache."""
+import pytest
+import torch
+
+import cache_reference as R
+from test_gpu_cache import DT, _cache, _ptr, _values
+
+pytestmark = pytest.mark.gpu
+
+
+# single tokens, few rows (one and two tiles of 16 columns), and bf16 sequences of more than 112 columns
+@pytest.mark.parametrize("dtype,hq,rows", [("bf16", 1, 1), ("bf16", 2, 3), ("f32", 2, 3), ("bf16", 8, 4), ("f32", 8, 4), ("bf16", 8, 30), ("bf16", 16, 70)])
+# among the last keys, in a step that only some rows see whole, and in one that all do
+@pytest.mark.parametrize("key", [299, 298, 290, 257, 256, 231, 200, 10])
+def test_a_nan_under_a_weight_of_zero_is_seen(dtype, hq, rows, key):
+    hkv, d, dt, n, scale = 1, 128, DT[dtype], 300, 0.125
+    # the cache holds 1.008 for 1: every score is 60 * 0.125 * 128 * 1.008 = 967, the spoilt key's -967: its weight is 0 in any type, e^-1935
+    k, v = torch.ones(n, hkv, d), _values((n, hkv, d), 2, dt).float()
+    k[key] = -1
+    v[key, 0, 5], v[key, 0, 100] = float("nan"), float("inf")                # groups 0 and 3
+    k, v = k.to(dt), v.to(dt)
+    c = _cache([n], hkv, d, dt, 16, max_rows=rows, hq=hq)
+    c.write(k.cuda(), v.cuda(), _ptr([n]))
+    q = torch.full((rows, hq, d), 60.0, dtype=dt)
+    o, lse = torch.empty(rows, hq, d, dtype=dt, device="cuda"), torch.empty(hq, rows, device="cuda")
+    c.attend(q.cuda(), o, lse, scale, _ptr([rows]))
+    sees = torch.arange(n - rows, n) >= key
+    nan = torch.isnan(o.float()).cpu()
+    spoilt = torch.zeros(d, dtype=torch.bool)
+    spoilt[:32] = spoilt[96:] = True
+    assert torch.equal(nan, (sees[:, None, None] & spoilt).expand(rows, hq, d))
+    clean = R.held(v)
+    clean[key] = 0                                         # what the other channels of the key add: 0 times a finite value
+    want, lse_want, size = R.attend(q, R.held(k), clean, hq, scale, n - rows)
+    u, E = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -20, 2.0 ** -18 * 970
+    err = (o.double().cpu() - want).abs()
+    assert (err <= u * size + u * want.abs() + 2 * E * size)[~nan].all()
+    assert ((lse.double().cpu() - lse_want).abs() <= E + 2.0 ** -20 * 1000).all()
