@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from functools import lru_cache
 from typing import Optional, Sequence, Tuple
@@ -530,7 +531,50 @@ def _explain(t, dtype, numel: int, what: str, dev: int) -> None:
         raise ValueError(f"{what}: {t.numel()} elements, expected {numel}")
     if t.get_device() != dev:
         raise ValueError(f"{what}: on {t.device}, expected the current GPU")
-    raise ValueError(f"{what}: tensor must be contiguous")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: tensor must be contiguous")
+
+
+def _vector_ptr(t, n: int, what: str, dev: int):
+    """Address of `n` floats, neither more nor fewer (one value per channel or pair: a longer one belongs to another shape)."""
+    if t is not None and type(t) is not int and t.numel() != n:
+        raise ValueError(f"{what}: {t.numel()} elements, expected {n}")
+    return _tensor_ptr(t, _torch_dtype(F32), n, what, dev)
+
+
+def _lines_ptr(t, dtype, lines: int, n: int, what: str, dev: int, more: bool = False):
+    """Address of `lines` lines of n elements, one behind the other (`more`: further lines may follow).  A single line may be longer."""
+    if t is None or type(t) is int:
+        return t
+    if t.shape != (lines, n) and lines > 1 and n > 0:
+        size = t.numel()
+        if (size < lines * n if more else size != lines * n) or (t.dim() > 1 and t.shape[-1] != n):
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(lines, n)}")
+    return _tensor_ptr(t, dtype, lines * n, what, dev)
+
+
+def _packed_ptr(t, n: int, heads: int, d: int, dtype, what: str, dev: int):
+    """Address of packed rows [n, heads, d] (further rows may follow; leading or head dimensions may be divided, heads and channels may be one
+    dimension, or all may be: the rows have to lie in memory as the library takes them)."""
+    if t is None or type(t) is int:
+        return t
+    if t.shape != (n, heads, d):
+        if t.numel() < n * heads * d:
+            _explain(t, dtype, n * heads * d, what, dev)
+        if t.dim() > 1 and not _has_rows(tuple(t.shape), n, heads, d):
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(n, heads, d)}")
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        _explain(t, dtype, 0, what, dev)
+    return t.data_ptr()
+
+
+def _has_rows(shape, n: int, heads: int, d: int) -> bool:
+    if shape[-1] != d and shape[-1] != heads * d:
+        return False
+    for i in range(1, len(shape)):
+        if math.prod(shape[i:]) == heads * d and (shape[0] >= n if i == 1 else math.prod(shape[:i]) == n):
+            return True
+    return False
 
 
 def _rows_ptr(t, T: int, heads: int, d: int, dtype, stride: int, what: str, dev: int):
@@ -570,15 +614,22 @@ def _rope_params(T, shape, q_stride=0, k_stride=0, dq_stride=0, dk_stride=0):
     return p, int(load_library().slimattn_rope_bwd_workspace_bytes(C.byref(p)))
 
 
+def _turns(rotary_dim, axes, T, positions, inv_freq, dev):
+    """Addresses (positions, inv_freq), which are not looked at without a rotation."""
+    if rotary_dim <= 0:
+        return None, None
+    return _lines_ptr(positions, _torch_dtype("int32"), axes, T, "positions", dev), _vector_ptr(inv_freq, rotary_dim // 2, "inv_freq", dev)
+
+
 def _rope_fwd(dev, stream, T, shape, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out, q_stride=0, k_stride=0):
     hq, hkv, d, dtype, rotary_dim, sections = shape[:6]
-    td, f32 = _torch_dtype(dtype), _torch_dtype(F32)
+    td = _torch_dtype(dtype)
     pq, q_stride = _rows_ptr(q, T, hq, d, td, q_stride, "q", dev)
     pk, k_stride = _rows_ptr(k, T, hkv, d, td, k_stride, "k", dev)
     rc = (_lib or load_library()).slimattn_rope_fwd(
-        _rope_params(T, shape, q_stride, k_stride)[0], pq, pk, _tensor_ptr(q_weight, f32, d, "q_weight", dev), _tensor_ptr(k_weight, f32, d, "k_weight", dev),
-        _tensor_ptr(positions, _torch_dtype("int32"), len(sections) * T, "positions", dev), _tensor_ptr(inv_freq, f32, rotary_dim // 2, "inv_freq", dev),
-        _tensor_ptr(q_out, td, T * d * hq, "q_out", dev), _tensor_ptr(k_out, td, T * d * hkv, "k_out", dev), stream)
+        _rope_params(T, shape, q_stride, k_stride)[0], pq, pk, _vector_ptr(q_weight, d, "q_weight", dev), _vector_ptr(k_weight, d, "k_weight", dev),
+        *_turns(rotary_dim, len(sections), T, positions, inv_freq, dev), _packed_ptr(q_out, T, hq, d, td, "q_out", dev),
+        _packed_ptr(k_out, T, hkv, d, td, "k_out", dev), stream)
     if rc != 0:
         _raise(rc, "slimattn_rope_fwd")
 
@@ -599,7 +650,7 @@ def rope_bwd_workspace_bytes(total_tokens: int, n_q_heads: int, n_kv_heads: int,
 def _rope_bwd(dev, stream, T, shape, q, k, positions, inv_freq, q_weight, k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, q_stride=0,
               k_stride=0, dq_stride=0, dk_stride=0):
     hq, hkv, d, dtype, rotary_dim, sections = shape[:6]
-    td, f32 = _torch_dtype(dtype), _torch_dtype(F32)
+    td = _torch_dtype(dtype)
     pq, q_stride = _rows_ptr(q, T, hq, d, td, q_stride, "q", dev)
     pk, k_stride = _rows_ptr(k, T, hkv, d, td, k_stride, "k", dev)
     pdq, dq_stride = _rows_ptr(dq, T, hq, d, td, dq_stride, "dq", dev)
@@ -608,10 +659,9 @@ def _rope_bwd(dev, stream, T, shape, q, k, positions, inv_freq, q_weight, k_weig
     if dq_weight is None and dk_weight is None:
         need = 0
     rc = (_lib or load_library()).slimattn_rope_bwd(
-        p, pq, pk, _tensor_ptr(q_weight, f32, d, "q_weight", dev), _tensor_ptr(k_weight, f32, d, "k_weight", dev),
-        _tensor_ptr(positions, _torch_dtype("int32"), len(sections) * T, "positions", dev), _tensor_ptr(inv_freq, f32, rotary_dim // 2, "inv_freq", dev),
-        _tensor_ptr(dq_out, td, T * d * hq, "dq_out", dev), _tensor_ptr(dk_out, td, T * d * hkv, "dk_out", dev), pdq, pdk,
-        _tensor_ptr(dq_weight, f32, d, "dq_weight", dev), _tensor_ptr(dk_weight, f32, d, "dk_weight", dev),
+        p, pq, pk, _vector_ptr(q_weight, d, "q_weight", dev), _vector_ptr(k_weight, d, "k_weight", dev),
+        *_turns(rotary_dim, len(sections), T, positions, inv_freq, dev), _packed_ptr(dq_out, T, hq, d, td, "dq_out", dev),
+        _packed_ptr(dk_out, T, hkv, d, td, "dk_out", dev), pdq, pdk, _vector_ptr(dq_weight, d, "dq_weight", dev), _vector_ptr(dk_weight, d, "dk_weight", dev),
         _tensor_ptr(workspace, _torch_dtype("uint8"), need, "workspace", dev), stream)
     if rc != 0:
         _raise(rc, "slimattn_rope_bwd")
@@ -646,7 +696,7 @@ def _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev):
     """Addresses (row_ptr, lens, page_table, cache), the tensors among them checked."""
     i32 = _torch_dtype("int32")
     return (_tensor_ptr(row_ptr, i32, p.n_seqs + 1, "row_ptr", dev), _tensor_ptr(lens, i32, p.n_seqs, "lens", dev),
-            _tensor_ptr(page_table, i32, p.n_seqs * p.max_pages, "page_table", dev), _tensor_ptr(cache, _torch_dtype("uint8"), size, "cache", dev))
+            _lines_ptr(page_table, i32, p.n_seqs, p.max_pages, "page_table", dev, more=True), _tensor_ptr(cache, _torch_dtype("uint8"), size, "cache", dev))
 
 
 def _cache_write(dev, stream, n_rows, shape, k, v, cache, page_table, lens, row_ptr, k_stride=0, v_stride=0):
@@ -667,10 +717,11 @@ def cache_write(k, v, cache, page_table, lens, row_ptr=None, *, n_rows: int, n_p
 
 
 def _cache_read(dev, stream, n_rows, shape, cache, page_table, lens, row_ptr, k, v):
-    td, n = _torch_dtype(shape[4]), n_rows * shape[2] * shape[3]
+    hkv, d, td = shape[2], shape[3], _torch_dtype(shape[4])
     p, size = _cache_params(shape, n_rows)
     rp, ln, pt, ca = _cache_arrays(p, size, cache, page_table, lens, row_ptr, dev)
-    rc = (_lib or load_library()).slimattn_cache_read(p, ca, rp, ln, pt, _tensor_ptr(k, td, n, "k", dev), _tensor_ptr(v, td, n, "v", dev), stream)
+    rc = (_lib or load_library()).slimattn_cache_read(p, ca, rp, ln, pt, _packed_ptr(k, n_rows, hkv, d, td, "k", dev), _packed_ptr(v, n_rows, hkv, d, td, "v", dev),
+                                                        stream)
     if rc != 0:
         _raise(rc, "slimattn_cache_read")
 
@@ -687,11 +738,11 @@ def cache_attn_workspace_bytes(n_q_heads: int, *, n_rows: int, n_pages: int, pag
 
 
 def _cache_attn(dev, stream, n_rows, shape, n_q_heads, scale, q, cache, page_table, lens, row_ptr, o, lse, workspace):
-    td, n = _torch_dtype(shape[4]), n_rows * n_q_heads * shape[3]
+    d, td = shape[3], _torch_dtype(shape[4])
     p, size = _cache_params(shape, n_rows)
     rc = (_lib or load_library()).slimattn_cache_attn(
-        p, n_q_heads, scale, _tensor_ptr(q, td, n, "q", dev), *_cache_arrays(p, size, cache, page_table, lens, row_ptr, dev), _tensor_ptr(o, td, n, "o", dev),
-        _tensor_ptr(lse, _torch_dtype(F32), n_rows * n_q_heads, "lse", dev),
+        p, n_q_heads, scale, _packed_ptr(q, n_rows, n_q_heads, d, td, "q", dev), *_cache_arrays(p, size, cache, page_table, lens, row_ptr, dev),
+        _packed_ptr(o, n_rows, n_q_heads, d, td, "o", dev), _lines_ptr(lse, _torch_dtype(F32), n_q_heads, n_rows, "lse", dev),
         _tensor_ptr(workspace, _torch_dtype("uint8"), _cache_attn_bytes(n_q_heads, shape, n_rows), "workspace", dev), stream)
     if rc != 0:
         _raise(rc, "slimattn_cache_attn")
