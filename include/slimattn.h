@@ -426,7 +426,7 @@ typedef struct slimattn_rope_params {
  * With SLIMATTN_ROPE_DEALT the axes take one pair each in turn, axis 0 first, as long as they have pairs left.  Angles are formed in
  * 64 bits and turned into (-pi/4, pi/4] before they are rounded: any int32 position is as exact as a small one.
  * q [T, Hq, d] by q_stride, k [T, Hkv, d] by k_stride -> q_out, k_out packed, as slimattn_fwd reads them.  q_weight, k_weight float [d]
- * (SLIMATTN_ROPE_NORM; NULL: ones); positions int32 [n_axes, T]; inv_freq float [rotary_dim / 2].  All DEVICE; tensors 16-byte
+ * (SLIMATTN_ROPE_NORM; NULL: ones; not read without a norm); positions int32 [n_axes, T]; inv_freq float [rotary_dim / 2].  All DEVICE; tensors 16-byte
  * aligned, the rest 4-byte.  q_out may be q (k_out be k) where that is packed; other overlaps of an output are refused.
  * A row whose sum of squares is beyond fp32 (or an infinity or a NaN in it) is NaN with SLIMATTN_ROPE_NORM, in all its channels.
  * Allocates nothing, does not synchronise, one kernel launch. */

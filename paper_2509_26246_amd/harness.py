@@ -128,6 +128,8 @@ class Rotary:
                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, norm: bool = False, eps: float = 1e-6,
                  rotary_dim: Optional[int] = None, sections: Optional[Sequence[int]] = None, dealt: bool = False, adjacent: bool = False,
                  device="cuda"):
+        if not norm and (q_weight is not None or k_weight is not None):
+            raise ValueError("q_weight, k_weight: weights of the norm, given without norm=True")
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         self.inv_freq, self.q_weight, self.k_weight, self.norm = inv_freq, q_weight, k_weight, norm
         rotary_dim = head_dim if rotary_dim is None else rotary_dim

@@ -5,6 +5,7 @@ import torch
 
 import paper_2509_26246_amd as S
 from paper_2509_26246_amd import binding as B
+from paper_2509_26246_amd import harness as H
 
 T, HQ, HKV, D = 8, 4, 2, 64
 ROPE = dict(total_tokens=T, n_q_heads=HQ, n_kv_heads=HKV, head_dim=D, dtype=S.F32, rotary_dim=D, sections=[16, 8, 8], flags=S.ROPE_NORM)
@@ -88,3 +89,11 @@ def test_ambiguous_heads_are_not_guessed():
     for shape in ((T, 2, D), (2, T, D), (T // 2, D), (T, 2 * D)):
         with pytest.raises(ValueError):
             B._packed_ptr(_f(*shape), T, 1, D, torch.float32, "x", -1)
+
+
+@pytest.mark.parametrize("weights", [dict(q_weight=_f(D)), dict(k_weight=_f(D)), dict(q_weight=_f(D), k_weight=_f(D))], ids=lambda w: "-".join(w))
+def test_weights_without_a_norm_are_refused(weights):
+    with pytest.raises(ValueError):
+        H.Rotary(HQ, HKV, D, torch.float32, _f(D // 2), device="cpu", **weights)
+    H.Rotary(HQ, HKV, D, torch.float32, _f(D // 2), norm=True, device="cpu", **weights)
+    H.Rotary(HQ, HKV, D, torch.float32, _f(D // 2), device="cpu")
