@@ -440,7 +440,7 @@ size_t slimattn_rope_bwd_workspace_bytes(const slimattn_rope_params* p);
 /* Gradients of slimattn_rope_fwd: dq_out [T, Hq, d], dk_out [T, Hkv, d] packed (as slimattn_bwd writes dQ, dK) -> dq, dk by dq_stride,
  * dk_stride, and with SLIMATTN_ROPE_NORM dq_weight, dk_weight float [d], summed over tokens and heads in a fixed order (no atomics; bitwise
  * repeatable) and overwritten; either may be NULL.  q, k are the inputs of the forward pass (read with SLIMATTN_ROPE_NORM only).
- * dq may be dq_out or q (dk be dk_out or k) where their strides are the same; other overlaps of an output are refused.
+ * dq may be dq_out or q (dk be dk_out or k) where their strides are the same; other overlaps of an output or the workspace are refused.
  * Allocates nothing, does not synchronise; one kernel launch, two with weight gradients. */
 int slimattn_rope_bwd(const slimattn_rope_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,
                       const int32_t* positions, const float* inv_freq, const void* dq_out, const void* dk_out, void* dq, void* dk,
@@ -473,7 +473,8 @@ typedef struct slimattn_cache_params {
  * are taken as 0 .. max_pages * page_size; a row at a negative position is not written, reads as zeros, and sees nothing (o = 0,
  * lse = -inf); a page index outside 0 .. n_pages - 1 is a page that is not there: not written, read as zeros, its keys not seen.  Rows before
  * row_ptr[0] and from row_ptr[n_seqs] on are left as they were.  Two rows of one call must not write the same position of a page.
- * All: 16-byte aligned tensors, cache and workspace; nothing allocated, no synchronisation, kernel launches only. */
+ * All: 16-byte aligned tensors, cache and workspace; nothing allocated, no synchronisation, kernel launches only.  What a call writes (its
+ * workspace too) must not overlap anything else of the call. */
 
 /* Bytes of the cache (DEVICE; needs no initialisation).  0 for a shape that the calls refuse. */
 size_t slimattn_cache_bytes(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
@@ -494,7 +495,7 @@ size_t slimattn_cache_attn_workspace_bytes(const slimattn_cache_params* p, int32
 
 /* Attention of the rows over their sequences' caches: the row at position p sees keys 0 .. p,
  * S_j = scale * q . k_j, lse = log sum_j exp S_j, o = sum_j exp(S_j - lse) v_j.  q, o [n_rows, Hq, d] packed, Hq a multiple of Hkv (query head h
- * uses KV head h / (Hq / Hkv)); lse float [Hq, n_rows] or NULL; o must not overlap q.  The keys of long sequences are divided among blocks
+ * uses KV head h / (Hq / Hkv)); lse float [Hq, n_rows] or NULL.  The keys of long sequences are divided among blocks
  * and the parts added in their order: the same call on the same inputs gives the same bits.  Sequences of more than 112 query columns (rows x Hq / Hkv) take a kernel of their own in
  * bf16, which only runs where n_rows allows for such a sequence: one, two or four launches.  An infinity or a NaN in a group of 32 channels
  * makes NaN of the rows that see its key (of a value: in those channels), and of no others. */

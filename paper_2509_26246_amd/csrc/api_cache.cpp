@@ -22,6 +22,12 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
+// Whether a call writes `out` over the arrays that it reads beside the tensors.
+bool over_arrays(const slimattn_cache_params* p, const void* out, int64_t n, const int32_t* row_ptr, const int32_t* lens, const int32_t* table) {
+  return overlap(out, n, lens, 4 * (int64_t)p->n_seqs) || overlap(out, n, table, 4 * (int64_t)p->n_seqs * p->max_pages) ||
+         overlap(out, n, row_ptr, row_ptr ? 4 * ((int64_t)p->n_seqs + 1) : 0);
+}
+
 bool geometry_ok(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t d) {
   if (n_pages < 1 || n_kv_heads < 1 || n_kv_heads > 65535 || (d != 64 && d != 128)) return false;
   return page_size == 16 || page_size == 32 || page_size == 64 || page_size == 128 || page_size == 256;
@@ -69,7 +75,9 @@ int slimattn_cache_write(const slimattn_cache_params* p, const void* k, const vo
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(cache, 16)) return SLIMATTN_EINVAL;
   const int64_t ks = k_stride ? k_stride : row, vs = v_stride ? v_stride : row;
   const int64_t bytes = (int64_t)slimattn_cache_bytes(p->n_pages, p->page_size, p->n_kv_heads, p->head_dim);
-  if (overlap(cache, bytes, k, ((p->n_rows - 1) * ks + row) * e) || overlap(cache, bytes, v, ((p->n_rows - 1) * vs + row) * e)) return SLIMATTN_EINVAL;
+  if (overlap(cache, bytes, k, ((p->n_rows - 1) * ks + row) * e) || overlap(cache, bytes, v, ((p->n_rows - 1) * vs + row) * e) ||
+      over_arrays(p, cache, bytes, row_ptr, lens, page_table))
+    return SLIMATTN_EINVAL;
   return hip_rc(launch_cache_write(*p, k, v, ks, vs, row_ptr, lens, page_table, cache, stream));
 }
 
@@ -83,7 +91,9 @@ int slimattn_cache_read(const slimattn_cache_params* p, const void* cache, const
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(cache, 16)) return SLIMATTN_EINVAL;
   const int64_t n = (int64_t)p->n_rows * p->n_kv_heads * p->head_dim * elem(p);
   const int64_t bytes = (int64_t)slimattn_cache_bytes(p->n_pages, p->page_size, p->n_kv_heads, p->head_dim);
-  if (overlap(k, n, v, n) || overlap(k, n, cache, bytes) || overlap(v, n, cache, bytes)) return SLIMATTN_EINVAL;
+  if (overlap(k, n, v, n) || overlap(k, n, cache, bytes) || overlap(v, n, cache, bytes) || over_arrays(p, k, n, row_ptr, lens, page_table) ||
+      over_arrays(p, v, n, row_ptr, lens, page_table))
+    return SLIMATTN_EINVAL;
   return hip_rc(launch_cache_read(*p, cache, row_ptr, lens, page_table, k, v, stream));
 }
 
@@ -102,7 +112,14 @@ int slimattn_cache_attn(const slimattn_cache_params* p, int32_t n_q_heads, float
   if (rc != SLIMATTN_OK) return rc;
   if (!aligned(q, 16) || !aligned(o, 16) || !aligned(cache, 16) || !aligned(workspace, 16) || (lse && !aligned(lse, 4))) return SLIMATTN_EINVAL;
   const int64_t n = (int64_t)p->n_rows * n_q_heads * p->head_dim * elem(p);
-  if (overlap(q, n, o, n)) return SLIMATTN_EINVAL;
+  const struct { const void* p; int64_t n; } out[] = {{o, n}, {lse, lse ? 4 * (int64_t)p->n_rows * n_q_heads : 0}, {workspace, (int64_t)cache_attn_bytes(*p, n_q_heads)}};
+  const int64_t bytes = (int64_t)slimattn_cache_bytes(p->n_pages, p->page_size, p->n_kv_heads, p->head_dim);
+  for (int i = 0; i < 3; ++i) {
+    if (overlap(out[i].p, out[i].n, q, n) || overlap(out[i].p, out[i].n, cache, bytes) || over_arrays(p, out[i].p, out[i].n, row_ptr, lens, page_table))
+      return SLIMATTN_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return SLIMATTN_EINVAL;
+  }
   return hip_rc(launch_cache_attn(*p, n_q_heads, scale, q, row_ptr, lens, page_table, cache, o, lse, workspace, stream));
 }
 

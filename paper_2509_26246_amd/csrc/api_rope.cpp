@@ -38,6 +38,18 @@ bool clash(const Rows& out, const Rows& x, int64_t T, bool same_ok) {
   return d < out.width || d + x.width > out.stride;
 }
 
+// A span of bytes, and whether rows (T of them) or another span share any of them.
+struct Span { const void* p; int64_t bytes; };
+
+bool touches(const Rows& x, int64_t T, const Span& s) {
+  if (!x.width || !s.p || s.bytes <= 0) return false;
+  const int64_t at = (int64_t)reinterpret_cast<uintptr_t>(s.p) - (int64_t)reinterpret_cast<uintptr_t>(x.p);
+  if (at + s.bytes <= 0 || at >= (T - 1) * x.stride + x.width) return false;
+  return at < 0 || at % x.stride < x.width || at % x.stride + s.bytes > x.stride;
+}
+
+bool touches(const Span& a, const Span& b) { return a.p && a.bytes > 0 && touches(Rows{a.p, a.bytes, a.bytes}, 1, b); }
+
 int check(const slimattn_rope_params* p) {
   if (!p || (p->dtype != SLIMATTN_F32 && p->dtype != SLIMATTN_BF16)) return SLIMATTN_EINVAL;
   const int d = p->head_dim;
@@ -75,6 +87,14 @@ bool small_inputs_ok(const slimattn_rope_params* p, const float* qw, const float
   return (!qw || aligned(qw, 4)) && (!kw || aligned(kw, 4));
 }
 
+// The arrays beside the tensors that a call reads.
+struct SmallInputs { Span s[4]; };
+SmallInputs small_inputs(const slimattn_rope_params* p, const float* qw, const float* kw, const int32_t* pos, const float* freq) {
+  const bool norm = p->flags & SLIMATTN_ROPE_NORM, turn = p->rotary_dim > 0;
+  const int64_t w = norm ? 4 * p->head_dim : 0;
+  return {{{qw, w}, {kw, w}, {pos, turn ? 4 * (int64_t)p->n_axes * p->total_tokens : 0}, {freq, turn ? 2 * p->rotary_dim : 0}}};
+}
+
 }  // namespace
 
 extern "C" {
@@ -92,6 +112,8 @@ int slimattn_rope_fwd(const slimattn_rope_params* p, const void* q, const void* 
   const Rows oq = rows(p, q_out, p->n_q_heads, 0), ok = rows(p, k_out, p->n_kv_heads, 0);
   if (clash(oq, rq, T, true) || clash(oq, rk, T, false) || clash(ok, rk, T, true) || clash(ok, rq, T, false) || clash(oq, ok, T, false))
     return SLIMATTN_EINVAL;
+  for (const Span& s : small_inputs(p, q_weight, k_weight, positions, inv_freq).s)
+    if (touches(oq, T, s) || touches(ok, T, s)) return SLIMATTN_EINVAL;
   return hip_rc(launch_rope_fwd(*p, q, k, q_weight, k_weight, positions, inv_freq, q_out, k_out, stream));
 }
 
@@ -107,6 +129,10 @@ int slimattn_rope_bwd(const slimattn_rope_params* p, const void* q, const void* 
   const int64_t T = p->total_tokens;
   const bool norm = p->flags & SLIMATTN_ROPE_NORM;
   if ((dq_weight && !aligned(dq_weight, 4)) || (dk_weight && !aligned(dk_weight, 4))) return SLIMATTN_EINVAL;
+  // what is written beside the tensors (nothing of it without a norm)
+  const int64_t w = norm ? 4 * p->head_dim : 0;
+  const Span dqw{dq_weight, w}, dkw{dk_weight, w}, ws{workspace, dq_weight || dk_weight ? (int64_t)slimattn_rope_bwd_workspace_bytes(p) : 0};
+  if (touches(dqw, dkw) || touches(dqw, ws) || touches(dkw, ws)) return SLIMATTN_EINVAL;
   if (T > 0) {
     if (p->n_q_heads && (!aligned(dq_out, 16) || !aligned(dq, 16) || (norm && !aligned(q, 16)))) return SLIMATTN_EINVAL;
     if (p->n_kv_heads && (!aligned(dk_out, 16) || !aligned(dk, 16) || (norm && !aligned(k, 16)))) return SLIMATTN_EINVAL;
@@ -118,6 +144,11 @@ int slimattn_rope_bwd(const slimattn_rope_params* p, const void* q, const void* 
     if (clash(oq, gq, T, true) || clash(oq, gk, T, false) || clash(ok, gk, T, true) || clash(ok, gq, T, false) || clash(oq, xq, T, true) ||
         clash(oq, xk, T, false) || clash(ok, xk, T, true) || clash(ok, xq, T, false) || clash(oq, ok, T, false))
       return SLIMATTN_EINVAL;
+    for (const Span& s : small_inputs(p, q_weight, k_weight, positions, inv_freq).s)
+      if (touches(oq, T, s) || touches(ok, T, s) || touches(dqw, s) || touches(dkw, s) || touches(ws, s)) return SLIMATTN_EINVAL;
+    for (const Span& s : {dqw, dkw, ws})
+      for (const Rows& x : {oq, ok, gq, gk, xq, xk})
+        if (touches(x, T, s)) return SLIMATTN_EINVAL;
   }
   return hip_rc(launch_rope_bwd(*p, q, k, q_weight, k_weight, positions, inv_freq, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace,
                                 stream));

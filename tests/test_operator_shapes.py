@@ -1,5 +1,6 @@
 """Tensors whose memory does not lie as the operators would read it are refused by their shapes, before a launch; those that lie so by another shape are
-taken.  Tensors of the CPU stand for the GPU's: no call here reaches a kernel."""
+taken; outputs that lie over anything else of the call are refused.  Tensors of the CPU stand for the GPU's, and addresses are never looked at: no call here
+reaches a kernel."""
 import pytest
 import torch
 
@@ -97,3 +98,62 @@ def test_weights_without_a_norm_are_refused(weights):
         H.Rotary(HQ, HKV, D, torch.float32, _f(D // 2), device="cpu", **weights)
     H.Rotary(HQ, HKV, D, torch.float32, _f(D // 2), norm=True, device="cpu", **weights)
     H.Rotary(HQ, HKV, D, torch.float32, _f(D // 2), device="cpu")
+
+
+A = 1 << 32
+
+
+def _overlaps_rope(call, over, **shape):
+    ptr = {n: (i + 1) * A for i, n in enumerate(("q", "k", "positions", "inv_freq", "q_out", "k_out", "dq", "dk", "dq_weight", "dk_weight", "workspace", "q_weight", "k_weight"))}
+    ptr.update({n: (ptr[v[0]] + v[1]) for n, v in over.items()})
+    kw = dict(ROPE, q_weight=ptr["q_weight"], k_weight=ptr["k_weight"], **shape)
+    first = [ptr[n] for n in ("q", "k", "positions", "inv_freq", "q_out", "k_out")]
+    with pytest.raises(S.SlimAttnError) as e:
+        S.rope_fwd(*first, **kw) if call == "fwd" else S.rope_bwd(*first, *[ptr[n] for n in ("dq", "dk", "dq_weight", "dk_weight", "workspace")], **kw)
+    assert e.value.code == -1
+
+
+ROW = HQ * D * 4                                           # bytes of a token's queries
+
+
+@pytest.mark.parametrize("over", [dict(positions=("q_out", 0)), dict(positions=("q_out", T * ROW - 4)), dict(positions=("q_out", -4)), dict(inv_freq=("k_out", 64)),
+                                  dict(q_weight=("q_out", 256)), dict(k_weight=("q_out", 4)), dict(k_weight=("k_out", -D * 4 + 4))], ids=str)
+def test_forward_refuses_outputs_over_its_other_inputs(over):
+    _overlaps_rope("fwd", over)
+
+
+@pytest.mark.parametrize("over", [dict(dk_weight=("dq_weight", 0)), dict(dk_weight=("dq_weight", D * 4 - 4)), dict(dq_weight=("dk_weight", 4)), dict(dq_weight=("workspace", 64)),
+                                  dict(workspace=("dk_weight", -1024)), dict(workspace=("dq", 0)), dict(workspace=("dk_out_", 0)), dict(workspace=("q", -4096)),
+                                  dict(dq_weight=("dq", ROW)), dict(dk_weight=("k", 0)), dict(dq_weight=("q_weight", 0)), dict(positions=("dq", 0)), dict(inv_freq=("dk", 8)),
+                                  dict(q_weight=("dq", 0)), dict(positions=("workspace", 0)), dict(dk_weight=("inv_freq", 0))], ids=str)
+def test_backward_refuses_outputs_over_anything(over):
+    _overlaps_rope("bwd", {n: ((v[0] if v[0] != "dk_out_" else "k_out"), v[1]) for n, v in over.items()})
+
+
+def test_rows_with_room_between_them():
+    # the gradients of a fused projection: what lies over a row is refused, also over the last one and over two at once
+    for at in (0, ROW - 4, 3 * ROW - 4, 3 * ROW, 7 * 3 * ROW + ROW - 4, ROW - D * 4 + 4, 3 * ROW - D * 4 + 4):
+        _overlaps_rope("bwd", dict(dq_weight=("dq", at)), dq_stride=3 * HQ * D)
+
+
+def _overlaps_cache(call, over):
+    ptr = {n: (i + 1) * A for i, n in enumerate(("k", "v", "cache", "page_table", "lens", "row_ptr", "q", "o", "lse", "workspace"))}
+    ptr.update({n: ptr[v[0]] + v[1] for n, v in over.items()})
+    with pytest.raises(S.SlimAttnError) as e:
+        if call == "write":
+            S.cache_write(ptr["k"], ptr["v"], ptr["cache"], ptr["page_table"], ptr["lens"], ptr["row_ptr"], **CACHE)
+        elif call == "read":
+            S.cache_read(ptr["cache"], ptr["page_table"], ptr["lens"], ptr["k"], ptr["v"], ptr["row_ptr"], **CACHE)
+        else:
+            S.cache_attn(*[ptr[n] for n in ("q", "cache", "page_table", "lens", "o", "lse", "workspace", "row_ptr")], n_q_heads=HQ, scale=0.1, **CACHE)
+    assert e.value.code == -1
+
+
+ARRAYS = [("lens", 0), ("lens", 12), ("page_table", 60), ("row_ptr", 16)]
+
+
+@pytest.mark.parametrize("call,over", [(call, {n: (out, 16 - at)}) for call, outs in (("write", ("cache",)), ("read", ("k", "v")), ("attn", ("o", "lse", "workspace"))) for out in outs for n, at in ARRAYS]
+                         + [("attn", o) for o in (dict(lse=("o", 4)), dict(lse=("q", 0)), dict(workspace=("o", 16)), dict(o=("workspace", 1024)), dict(lse=("workspace", 0)),
+                                                  dict(workspace=("q", 0)), dict(workspace=("cache", 0)), dict(o=("cache", 64)), dict(lse=("cache", 0)), dict(o=("q", 16)))], ids=str)
+def test_cache_calls_refuse_outputs_over_anything(call, over):
+    _overlaps_cache(call, over)
