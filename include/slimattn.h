@@ -423,8 +423,8 @@ typedef struct slimattn_rope_params {
 /* Norm of every query and key head, then rotation by the token's positions, in one pass over the tensors:
  *   n_c = x_c * w_c / sqrt(mean_c x_c^2 + eps)                         (SLIMATTN_ROPE_NORM; otherwise n = x)
  *   (a, b) of pair i  ->  (a cos t - b sin t, b cos t + a sin t),  t = positions[axis of pair i][token] * inv_freq[i].
- * With SLIMATTN_ROPE_DEALT the axes take one pair each in turn, axis 0 first, as long as they have pairs left.  Angles are formed in
- * 64 bits and turned into (-pi/4, pi/4] before they are rounded: any int32 position is as exact as a small one.
+ * With SLIMATTN_ROPE_DEALT the axes take one pair each in turn, axis 0 first, as long as they have pairs left.  Angles are formed
+ * exactly and turned into [-pi/4, pi/4] before they are rounded: any int32 position is as exact as a small one (sines and cosines within 2^-23).
  * q [T, Hq, d] by q_stride, k [T, Hkv, d] by k_stride -> q_out, k_out packed, as slimattn_fwd reads them.  q_weight, k_weight float [d]
  * (SLIMATTN_ROPE_NORM; NULL: ones; not read without a norm); positions int32 [n_axes, T]; inv_freq float [rotary_dim / 2].  All DEVICE; tensors 16-byte
  * aligned, the rest 4-byte.  q_out may be q (k_out be k) where that is packed; other overlaps of an output are refused.

@@ -12,8 +12,9 @@
 // A head takes d/8 lanes, a wave 64 / (d/8) heads; the lanes of one head ("group") keep a token and walk its heads, so the four
 // sines and cosines of a lane are computed once per token and not once per head.  Few tokens are divided by heads as well.
 //
-// Angles: position * frequency (31 x 24 bits) is formed in 64 bits, reduced there to a quarter turn around zero and only then rounded:
-// in 32 bits a position of 10^6 would be off by 0.03 rad.  Sine and cosine of at most pi/4 are their Taylor sums (the first term left
+// Angles: position * frequency (31 x 24 bits) and its turns are formed exactly, as two 64-bit numbers, and reduced to a quarter turn around zero before they
+// are rounded to 32 bits, so that far positions lose nothing: in 32 bits a position of 10^6 would be off by 0.03 rad, in one 64-bit number one of 2^31
+// by 4e-7, several times what rounding the reduced angle costs.  Sine and cosine of at most pi/4 are their Taylor sums (the first term left
 // out is below 2e-9), which costs less than the general functions' own reduction.
 #include <hip/hip_runtime.h>
 
@@ -44,10 +45,15 @@ __device__ __forceinline__ int first_pair(int j) { return 4 * j; }
 
 struct Turn { float c[4], s[4]; };
 
-// Sine and cosine of pos * freq.  u: turns, |fraction| reduced to an eighth around the nearest quarter turn.
+// Sine and cosine of pos * freq.  u + lo: turns (the product with its remainder, times 1 / 2 pi in two words: off by less than 2^-100 of them); their fraction
+// is reduced to an eighth around the nearest quarter turn.
 __device__ __forceinline__ void turn_of(int pos, float freq, float& c, float& s) {
-  const double u = (double)pos * (double)freq * 0.15915494309189533577;
-  const double f = u - __builtin_rint(u);
+#pragma clang fp contract(off)   // (u itself is what lo completes)
+  constexpr double kTurn = 0.15915494309189535, kTurnLow = -9.839338337591243e-18;
+  const double p = (double)pos * (double)freq, u = p * kTurn;
+  const double lo = __builtin_fma(__builtin_fma((double)pos, (double)freq, -p), kTurn, __builtin_fma(p, kTurnLow, __builtin_fma(p, kTurn, -u)));
+  double f = (u - __builtin_rint(u)) + lo;
+  f -= __builtin_rint(f);
   const double k = __builtin_rint(4.0 * f);
   const float a = (float)((f - 0.25 * k) * 6.283185307179586477);
   const int quarter = (int)k & 3;
