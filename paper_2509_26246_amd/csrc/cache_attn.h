@@ -1,6 +1,7 @@
 // Attention over the 4-bit cache: what its kernels share -- the row of work that a launch divides evenly among its blocks, whatever the lengths
 // are, and the list of items whose parts have to be added up afterwards.
 #pragma once
+#include "block_order.h"
 #include "cache.h"
 
 namespace slimattn {
@@ -70,17 +71,17 @@ __device__ __forceinline__ long long block_scan(long long x, long long* lds, lon
 // The block that holds unit x of U, when block i of n holds units [U i / n, U (i + 1) / n).
 __device__ __forceinline__ int block_of(long long x, long long U, int n) { return (int)(((x + 1) * n - 1) / U); }
 
-// Block `id` of at most N: units [begin, end) of `total`, divided among `blocks` blocks; the sequence in which it begins, with the units and
+// Piece `id` of the work: units [begin, end) of `total`, divided among `blocks` blocks; the sequence in which it begins, with the units and
 // items before that sequence.
 struct Place {
   long long total, begin, end, seq_begin, seq_item;
-  int blocks, seq;
+  int blocks, id, seq;
 };
 
 // Row: what a sequence adds (units_of_all(), items()), and how many blocks share a row of so much work.  False: nothing to do for this block.
 // As many sequences as the block has threads are one look at the lengths.
 template <class Row, int THREADS>
-__device__ __forceinline__ bool find_place(const AttnArgs& a, int N, int id, long long* scan, long long* found, Header* header, Place& p) {
+__device__ __forceinline__ bool find_place(const AttnArgs& a, long long* scan, long long* found, Header* header, Place& p) {
   const int tid = threadIdx.x;
   const bool one_look = a.c.n_seqs <= THREADS, with_items = Row::kNeedsItems || a.slots;
   long long mine = 0, my_items = 0, items = 0;
@@ -90,11 +91,12 @@ __device__ __forceinline__ bool find_place(const AttnArgs& a, int N, int id, lon
     my_items += s.items();
   }
   const long long units_to = block_scan<THREADS>(mine, scan, p.total), items_to = with_items ? block_scan<THREADS>(my_items, scan, items) : 0;
-  p.blocks = Row::blocks(a, N, p.total, items);
+  p.blocks = Row::blocks(a, (int)gridDim.x, p.total, items);
   if (blockIdx.x == 0 && tid == 0) header->listed = a.slots ? (int)min((long long)a.slots, items) : p.blocks;
-  if (id >= p.blocks) return false;
-  p.begin = p.total * id / p.blocks;
-  p.end = p.total * (id + 1) / p.blocks;
+  if ((int)blockIdx.x >= p.blocks) return false;
+  p.id = piece_of_block(blockIdx.x, p.blocks);
+  p.begin = p.total * p.id / p.blocks;
+  p.end = p.total * (p.id + 1) / p.blocks;
   if (one_look) {
     if (p.begin < units_to && p.begin >= units_to - mine) { found[0] = tid; found[1] = units_to - mine; found[2] = items_to - my_items; }
   } else {

@@ -300,13 +300,10 @@ __global__ __launch_bounds__(kThreads, (kBlocksPerCu<D, TERMS>)) void cache_attn
   __shared__ __align__(16) char lds[kLds<D>];
   __shared__ long long scan[kWaves], found[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 4, col = lane & 15;
-  const int N = gridDim.x;
-  // neighbouring blocks of the row of units on one XCD: tiles of one head read the same keys
-  const int id = N % 8 == 0 ? (int)(blockIdx.x % 8) * (N / 8) + blockIdx.x / 8 : blockIdx.x;
 
   Place place;
-  if (!find_place<NarrowRow, kThreads>(a, N, id, scan, found, split_header(ws), place)) return;
-  const int n = place.blocks;
+  if (!find_place<NarrowRow, kThreads>(a, scan, found, split_header(ws), place)) return;
+  const int n = place.blocks, id = place.id;
   const long long U = place.total, u0 = place.begin, u1 = place.end;
   int b = place.seq;
   long long seq_begin = place.seq_begin, seq_item = place.seq_item;

@@ -217,11 +217,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a
   __shared__ long long scan[kWaves], found[3];
   LDS_PTR(char) lds = (LDS_PTR(char))smem;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
-  const int N = gridDim.x;
-  const int id = N % 8 == 0 ? (int)(blockIdx.x % 8) * (N / 8) + blockIdx.x / 8 : blockIdx.x;   // neighbours in the row of work on one XCD
   Header* header = split_header(ws + kListBytes);
   Place place;
-  if (!find_place<WideRow, kThreads>(a, N, id, scan, found, header, place)) return;
+  if (!find_place<WideRow, kThreads>(a, scan, found, header, place)) return;
+  const int id = place.id;
   int b = place.seq;
   long long seq_begin = place.seq_begin, seq_item = place.seq_item;
   WideRow s(a, b);

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import cache_reference as R
-from test_gpu_cache import DT, _cache, _ptr, _values
+from test_gpu_cache import DT, _cache, _check_attend, _ptr, _values
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,18 @@ def test_a_nan_under_a_weight_of_zero_is_seen(dtype, hq, rows, key):
     err = (o.double().cpu() - want).abs()
     assert (err <= u * size + u * want.abs() + 2 * E * size)[~nan].all()
     assert ((lse.double().cpu() - lse_want).abs() <= E + 2.0 ** -20 * 1000).all()
+
+
+@pytest.mark.parametrize("dtype,hq,lens,rows", [("bf16", 8, [700, 1, 2000], [1, 1, 1]), ("f32", 4, [300] * 9, [1] * 9), ("bf16", 8, [500, 130], [40, 30]),
+                                                ("bf16", 4, [260] * 40, [1] * 40), ("bf16", 16, [3000], [100]), ("bf16", 8, [64], [1])])
+def test_tables_with_room_to_grow(dtype, hq, lens, rows):
+    # many more blocks are launched than have work: which of them work, and on what, goes by the lengths
+    hkv, d, dt, page, scale = 1, 128, DT[dtype], 16, 0.09
+    c = _cache(lens, hkv, d, dt, page, max_rows=sum(rows), hq=hq, more_columns=4096)
+    k, v = _values((sum(lens), hkv, d), 1, dt), _values((sum(lens), hkv, d), 2, dt)
+    c.write(k.cuda(), v.cuda(), _ptr(lens))
+    q = _values((sum(rows), hq, d), 3, dt, False)
+    o, lse = torch.empty(sum(rows), hq, d, dtype=dt, device="cuda"), torch.empty(hq, sum(rows), device="cuda")
+    for _ in range(2):
+        c.attend(q.cuda(), o, lse, scale, _ptr(rows))
+        _check_attend(o, lse, q, R.held(k), R.held(v), lens, rows, hq, scale, dt)
