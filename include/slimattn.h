@@ -470,7 +470,7 @@ typedef struct slimattn_cache_params {
  *                                   n rows the i-th stands at position lens[b] - n + i.  Ascending.  NULL: one row each (n_rows = n_seqs);
  *   page_table [n_seqs, max_pages]  page_table[b][j] holds positions j * page_size ... of sequence b.  Entries past its length are not read.
  * Their contents cannot be checked before a launch.  Whatever they hold, nothing outside the tensors and the cache is touched: lengths
- * are taken as 0 .. max_pages * page_size; a row at a negative position is not written, reads as zeros, and sees nothing (o = 0,
+ * are taken as 0 .. max_pages * page_size, rows as 0 .. n_rows (a sequence's rows end with the tensors'); a row at a negative position is not written, reads as zeros, and sees nothing (o = 0,
  * lse = -inf); a page index outside 0 .. n_pages - 1 is a page that is not there: not written, read as zeros, its keys not seen.  Rows before
  * row_ptr[0] and from row_ptr[n_seqs] on are left as they were.  Two rows of one call must not write the same position of a page.
  * All: 16-byte aligned tensors, cache and workspace; nothing allocated, no synchronisation, kernel launches only.  What a call writes (its

@@ -60,10 +60,11 @@ __device__ __forceinline__ int wave_find_seq(const CacheView& c, int row) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Position of a row in its sequence (uniform): negative where the sequence is shorter than its rows, or where the row is nobody's.
+// Position of a row in its sequence (uniform): negative where the sequence is shorter than its rows, or where the row is nobody's.  A sequence's rows end
+// with the tensors', wherever row_ptr does (as in seq_rows of the attention).
 __device__ __forceinline__ int row_position(const CacheView& c, int row, int b) {
   if (!c.row_ptr) return seq_len(c, b) - 1;
-  const int r0 = c.row_ptr[b], r1 = c.row_ptr[b + 1];
+  const int r0 = c.row_ptr[b], r1 = min(c.row_ptr[b + 1], c.n_rows);
   return row < r0 || row >= r1 ? INT32_MIN : seq_len(c, b) - (r1 - row);
 }
 

@@ -54,3 +54,28 @@ def test_tables_with_room_to_grow(dtype, hq, lens, rows):
     for _ in range(2):
         c.attend(q.cuda(), o, lse, scale, _ptr(rows))
         _check_attend(o, lse, q, R.held(k), R.held(v), lens, rows, hq, scale, dt)
+
+
+@pytest.mark.parametrize("dtype,hq,more", [("bf16", 4, 5), ("f32", 4, 5), ("bf16", 16, 40), ("bf16", 4, 1 << 20)])
+def test_rows_beyond_the_tensors_are_no_rows(dtype, hq, more):
+    # row_ptr ends behind the tensors' last row: the last sequence has the rows up to there, at the positions before its end, for every call alike
+    hkv, d, dt, rows, lens, scale = 2, 64, DT[dtype], [3, 50], [40, 90], 0.125
+    n = sum(rows)
+    c = _cache(lens, hkv, d, dt, 16, max_rows=n, hq=hq)
+    k, v = _values((sum(lens), hkv, d), 1, dt), _values((sum(lens), hkv, d), 2, dt)
+    c.write(k.cuda(), v.cuda(), _ptr(lens))
+    beyond = torch.tensor([0, 3, n + more], dtype=torch.int32).cuda()
+    last = torch.cat([torch.arange(37, 40), torch.arange(40 + 40, 40 + 90)])
+    out = [torch.empty(n, hkv, d, dtype=dt, device="cuda") for _ in range(2)]
+    c.read(*out, beyond)
+    for got, x in zip(out, (k, v)):
+        assert torch.equal(got.double().cpu(), R.held(x)[last])
+    q = _values((n, hq, d), 3, dt, False)
+    o, lse = torch.empty(n, hq, d, dtype=dt, device="cuda"), torch.empty(hq, n, device="cuda")
+    c.attend(q.cuda(), o, lse, scale, beyond)
+    _check_attend(o, lse, q, R.held(k), R.held(v), lens, rows, hq // hkv, scale, dt)
+    new = [_values((n, hkv, d), s, dt) for s in (7, 8)]
+    c.write(*[x.cuda() for x in new], beyond)
+    c.read(*out, _ptr(rows))
+    for got, x in zip(out, new):
+        assert torch.equal(got.double().cpu(), R.held(x))
