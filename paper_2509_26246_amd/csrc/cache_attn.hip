@@ -585,8 +585,10 @@ int launch_cache_attn(const slimattn_cache_params& p, int n_q_heads, float scale
   const long long items = most_items(p, n_q_heads);
   a.slots = items < blocks ? (int)items : 0;
   const dim3 join(a.slots ? a.slots : blocks, a.slots && a.slots <= 64 ? kCols : 4);
-  // 32 parts of an item or more: 1024 threads, so that each adds up a few (four items of 131072 keys 27.1 -> 26.6 us in all; fewer parts gain nothing).
-  const bool many = a.slots && blocks >= 32 * a.slots;
+  // 128 parts of an item or more: 1024 threads, so that each adds up a few.  us in all with 256 / 1024 threads, bf16, d 128, 8 heads over one: one, two, four
+  // sequences of 131072 keys (512, 384, 192 parts each) 22.8 / 20.9, 25.3 / 24.0, 28.4 / 27.8; with fewer parts the larger blocks cost more than they
+  // save: eight of 131072 (96) 39.4 / 39.8, sixteen of 32768 (48) 26.0 / 26.6, fp32 of 65536 keys over 8 heads of 64 (96) 23.5 / 24.6.
+  const bool many = a.slots && blocks >= 128 * a.slots;
   // Where sequences have 16 columns or fewer on average, their keys are read by one tile each and by nobody before the next call, with the other
   // layers' caches in between: streamed.  Caches in rotation, d 128, 32 heads over 8, us without / with: 19 MB 18.4 / 17.3, 76 MB 27.4 / 25.4, 303 MB
   // 76.9 / 65.9, 606 MB 133 / 115; 64 columns a sequence (four tiles) 222 / 229; a single cache read again and again from the last-level

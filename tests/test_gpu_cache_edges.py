@@ -79,3 +79,21 @@ def test_rows_beyond_the_tensors_are_no_rows(dtype, hq, more):
     c.read(*out, _ptr(rows))
     for got, x in zip(out, new):
         assert torch.equal(got.double().cpu(), R.held(x))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,lens", [("bf16", 8, 1, 128, [40000]), ("bf16", 5, 1, 64, [34000]), ("f32", 8, 1, 128, [36000]), ("f32", 2, 2, 64, [70001]),
+                                                 ("bf16", 8, 1, 128, [70000, 33000])])
+def test_hundreds_of_parts(dtype, hq, hkv, d, lens):
+    # one item's keys over 130 to 280 blocks, whose parts a block of 1024 threads adds up: lists filled with ones before, the same bits each time
+    dt, n, scale = DT[dtype], len(lens), d ** -0.5
+    c = _cache(lens, hkv, d, dt, 64, max_rows=n, hq=hq)
+    k, v = _values((sum(lens), hkv, d), 1, dt), _values((sum(lens), hkv, d), 2, dt)
+    c.write(k.cuda(), v.cuda(), _ptr(lens))
+    q = _values((n, hq, d), 3, dt, False)
+    o, lse = torch.empty(n, hq, d, dtype=dt, device="cuda"), torch.empty(hq, n, device="cuda")
+    c.attend(q.cuda(), o, lse, scale)
+    _check_attend(o, lse, q, R.held(k), R.held(v), lens, [1] * n, hq // hkv, scale, dt)
+    again, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    c.workspace.fill_(0xFF)
+    c.attend(q.cuda(), again, lse2, scale)
+    assert torch.equal(o, again) and torch.equal(lse, lse2)
