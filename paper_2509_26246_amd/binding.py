@@ -535,18 +535,19 @@ def _explain(t, dtype, numel: int, what: str, dev: int) -> None:
         raise ValueError(f"{what}: tensor must be contiguous")
 
 
-def _vector_ptr(t, n: int, what: str, dev: int):
+def _vector_ptr(t, n: int, f32, what: str, dev: int):
     """Address of `n` floats, neither more nor fewer (one value per channel or pair: a longer one belongs to another shape)."""
-    if t is not None and type(t) is not int and t.numel() != n:
+    if t is None or type(t) is int:
+        return t
+    if t.numel() != n or t.dtype is not f32 or t.get_device() != dev or not t.is_contiguous():
+        _explain(t, f32, n, what, dev)
         raise ValueError(f"{what}: {t.numel()} elements, expected {n}")
-    return _tensor_ptr(t, _torch_dtype(F32), n, what, dev)
+    return t.data_ptr()
 
 
 def _lines_ptr(t, dtype, lines: int, n: int, what: str, dev: int, more: bool = False):
     """Address of `lines` lines of n elements, one behind the other (`more`: further lines may follow).  A single line may be longer."""
-    if t is None or type(t) is int:
-        return t
-    if t.shape != (lines, n) and lines > 1 and n > 0:
+    if lines > 1 and n > 0 and t is not None and type(t) is not int and t.shape != (lines, n):
         size = t.numel()
         if (size < lines * n if more else size != lines * n) or (t.dim() > 1 and t.shape[-1] != n):
             raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(lines, n)}")
@@ -614,21 +615,15 @@ def _rope_params(T, shape, q_stride=0, k_stride=0, dq_stride=0, dk_stride=0):
     return p, int(load_library().slimattn_rope_bwd_workspace_bytes(C.byref(p)))
 
 
-def _turns(rotary_dim, axes, T, positions, inv_freq, dev):
-    """Addresses (positions, inv_freq), which are not looked at without a rotation."""
-    if rotary_dim <= 0:
-        return None, None
-    return _lines_ptr(positions, _torch_dtype("int32"), axes, T, "positions", dev), _vector_ptr(inv_freq, rotary_dim // 2, "inv_freq", dev)
-
-
 def _rope_fwd(dev, stream, T, shape, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out, q_stride=0, k_stride=0):
     hq, hkv, d, dtype, rotary_dim, sections = shape[:6]
-    td = _torch_dtype(dtype)
+    td, f32, turned = _torch_dtype(dtype), _torch_dtype(F32), rotary_dim > 0       # (positions and frequencies are not looked at without a rotation)
     pq, q_stride = _rows_ptr(q, T, hq, d, td, q_stride, "q", dev)
     pk, k_stride = _rows_ptr(k, T, hkv, d, td, k_stride, "k", dev)
     rc = (_lib or load_library()).slimattn_rope_fwd(
-        _rope_params(T, shape, q_stride, k_stride)[0], pq, pk, _vector_ptr(q_weight, d, "q_weight", dev), _vector_ptr(k_weight, d, "k_weight", dev),
-        *_turns(rotary_dim, len(sections), T, positions, inv_freq, dev), _packed_ptr(q_out, T, hq, d, td, "q_out", dev),
+        _rope_params(T, shape, q_stride, k_stride)[0], pq, pk, _vector_ptr(q_weight, d, f32, "q_weight", dev), _vector_ptr(k_weight, d, f32, "k_weight", dev),
+        _lines_ptr(positions if turned else None, _torch_dtype("int32"), len(sections), T, "positions", dev),
+        _vector_ptr(inv_freq if turned else None, rotary_dim // 2, f32, "inv_freq", dev), _packed_ptr(q_out, T, hq, d, td, "q_out", dev),
         _packed_ptr(k_out, T, hkv, d, td, "k_out", dev), stream)
     if rc != 0:
         _raise(rc, "slimattn_rope_fwd")
@@ -650,7 +645,7 @@ def rope_bwd_workspace_bytes(total_tokens: int, n_q_heads: int, n_kv_heads: int,
 def _rope_bwd(dev, stream, T, shape, q, k, positions, inv_freq, q_weight, k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, q_stride=0,
               k_stride=0, dq_stride=0, dk_stride=0):
     hq, hkv, d, dtype, rotary_dim, sections = shape[:6]
-    td = _torch_dtype(dtype)
+    td, f32, turned = _torch_dtype(dtype), _torch_dtype(F32), rotary_dim > 0       # (positions and frequencies are not looked at without a rotation)
     pq, q_stride = _rows_ptr(q, T, hq, d, td, q_stride, "q", dev)
     pk, k_stride = _rows_ptr(k, T, hkv, d, td, k_stride, "k", dev)
     pdq, dq_stride = _rows_ptr(dq, T, hq, d, td, dq_stride, "dq", dev)
@@ -659,9 +654,10 @@ def _rope_bwd(dev, stream, T, shape, q, k, positions, inv_freq, q_weight, k_weig
     if dq_weight is None and dk_weight is None:
         need = 0
     rc = (_lib or load_library()).slimattn_rope_bwd(
-        p, pq, pk, _vector_ptr(q_weight, d, "q_weight", dev), _vector_ptr(k_weight, d, "k_weight", dev),
-        *_turns(rotary_dim, len(sections), T, positions, inv_freq, dev), _packed_ptr(dq_out, T, hq, d, td, "dq_out", dev),
-        _packed_ptr(dk_out, T, hkv, d, td, "dk_out", dev), pdq, pdk, _vector_ptr(dq_weight, d, "dq_weight", dev), _vector_ptr(dk_weight, d, "dk_weight", dev),
+        p, pq, pk, _vector_ptr(q_weight, d, f32, "q_weight", dev), _vector_ptr(k_weight, d, f32, "k_weight", dev),
+        _lines_ptr(positions if turned else None, _torch_dtype("int32"), len(sections), T, "positions", dev),
+        _vector_ptr(inv_freq if turned else None, rotary_dim // 2, f32, "inv_freq", dev), _packed_ptr(dq_out, T, hq, d, td, "dq_out", dev),
+        _packed_ptr(dk_out, T, hkv, d, td, "dk_out", dev), pdq, pdk, _vector_ptr(dq_weight, d, f32, "dq_weight", dev), _vector_ptr(dk_weight, d, f32, "dk_weight", dev),
         _tensor_ptr(workspace, _torch_dtype("uint8"), need, "workspace", dev), stream)
     if rc != 0:
         _raise(rc, "slimattn_rope_bwd")
