@@ -79,9 +79,9 @@ struct Place {
 };
 
 // Row: what a sequence adds (units_of_all(), items()), and how many blocks share a row of so much work.  False: nothing to do for this block.
-// As many sequences as the block has threads are one look at the lengths.
+// As many sequences as the block has threads are one look at the lengths.  N: the launch's blocks.
 template <class Row, int THREADS>
-__device__ __forceinline__ bool find_place(const AttnArgs& a, long long* scan, long long* found, Header* header, Place& p) {
+__device__ __forceinline__ bool find_place(const AttnArgs& a, int N, long long* scan, long long* found, Header* header, Place& p) {
   const int tid = threadIdx.x;
   const bool one_look = a.c.n_seqs <= THREADS, with_items = Row::kNeedsItems || a.slots;
   long long mine = 0, my_items = 0, items = 0;
@@ -91,7 +91,7 @@ __device__ __forceinline__ bool find_place(const AttnArgs& a, long long* scan, l
     my_items += s.items();
   }
   const long long units_to = block_scan<THREADS>(mine, scan, p.total), items_to = with_items ? block_scan<THREADS>(my_items, scan, items) : 0;
-  p.blocks = Row::blocks(a, (int)gridDim.x, p.total, items);
+  p.blocks = Row::blocks(a, N, p.total, items);
   if (blockIdx.x == 0 && tid == 0) header->listed = a.slots ? (int)min((long long)a.slots, items) : p.blocks;
   if ((int)blockIdx.x >= p.blocks) return false;
   p.id = piece_of_block(blockIdx.x, p.blocks);

@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_wide_kernel(AttnArgs a
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
   Header* header = split_header(ws + kListBytes);
   Place place;
-  if (!find_place<WideRow, kThreads>(a, scan, found, header, place)) return;
+  if (!find_place<WideRow, kThreads>(a, (int)gridDim.x, scan, found, header, place)) return;
   const int id = place.id;
   int b = place.seq;
   long long seq_begin = place.seq_begin, seq_item = place.seq_item;
