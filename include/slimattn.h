@@ -496,8 +496,9 @@ size_t slimattn_cache_attn_workspace_bytes(const slimattn_cache_params* p, int32
 /* Attention of the rows over their sequences' caches: the row at position p sees keys 0 .. p,
  * S_j = scale * q . k_j, lse = log sum_j exp S_j, o = sum_j exp(S_j - lse) v_j.  q, o [n_rows, Hq, d] packed, Hq a multiple of Hkv (query head h
  * uses KV head h / (Hq / Hkv)); lse float [Hq, n_rows] or NULL.  The keys of long sequences are divided among blocks
- * and the parts added in their order: the same call on the same inputs gives the same bits.  Sequences of more than 112 query columns (rows x Hq / Hkv) take a kernel of their own in
- * bf16, which only runs where n_rows allows for such a sequence: one, two or four launches.  An infinity or a NaN in a group of 32 channels
+ * and the parts added in their order: the same call on the same inputs gives the same bits.  Statistics and sums are fp32; with SLIMATTN_BF16 the probabilities
+ * (times the values' scales) are rounded to bf16 for the product with the values, as in slimattn_fwd: o is within 2^-8 of the largest |v| by that, beside its own rounding.  Sequences of
+ * more than 112 query columns (rows x Hq / Hkv) take a kernel of their own in bf16, which only runs where n_rows allows for such a sequence: one, two or four launches.  An infinity or a NaN in a group of 32 channels
  * makes NaN of the rows that see its key (of a value: in those channels), and of no others. */
 int slimattn_cache_attn(const slimattn_cache_params* p, int32_t n_q_heads, float scale, const void* q, const int32_t* row_ptr,
                         const int32_t* lens, const int32_t* page_table, const void* cache, void* o, float* lse, void* workspace,

@@ -2,16 +2,21 @@
 //
 // Mathematics.  S = K q over the codes: the 32 channels of a scale group are one 16x16x32 product, whose 16 keys x 16 query columns are then
 // multiplied by the keys' scales in fp32 and added up over the groups: no value of K is ever formed, and q enters as it is.  Likewise
-// O^T = V^T P^T takes V's codes as they are, and the probabilities of a scale group times that group's scales (rounded to bf16 as P would
-// be).  fp32 calls hand q and P over as three bf16 terms, 24 bits: with exact codes the products are then as good as fp32 ones.
+// O^T = V^T P^T takes V's codes as they are, and the probabilities of a scale group times that group's scales.
 // Softmax statistics and sums are fp32, in log2 units; the maximum moves with every step.
+//
+// Fewer bits.  bf16 calls round probability times scale to bf16, the only rounding beside the output's: at most 2^-8 of each term, with either sign, so that an
+// output is off by 2.3e-3 of itself where rounding it alone costs 1.65e-3.  A second bf16 term of P (16 bits) gives 1.65e-3 and takes a product more and the
+// packing: 64 sequences of up to 4096 keys, 32 heads over 8, 53.6 -> 64.6 us, four of 131072 30.9 -> 36.4.  Not taken: slimattn_fwd rounds P
+// alike.  fp32 calls hand q and P over as three bf16 terms, 24 bits: with exact codes the products are then as good as fp32 ones.
 //
 // Bound by memory (144 bytes per key and KV head at head dim 128 against 4 * 128 flops per query head), so what counts is that every compute unit reads
 // all the time, whatever the lengths are.  The columns of a sequence's KV head (rows x heads of the group) are cut into tiles of 16, an item is
 // one tile's walk over the keys it sees, its length counted in units of 256 keys; the units of all items in a row are divided evenly among
 // the blocks of one launch, which find their place in that row by a scan over the lengths (they are data: a recorded call follows
 // them).  A block's first and last item may be parts; parts leave O, maximum and sum in the workspace, and a second launch adds them up in the
-// order of the keys (done by the same launch, its last blocks would have to wait for the others' parts behind counters that something has to clear).
+// order of the keys: the end of a launch is what makes the parts of eight XCDs visible to one block.  (The block that arrives last could add them up within the
+// launch, with parts stored for the whole device and a counter that it sets back; not built, so not measured.)
 // Measured, bf16, d 128: 64 sequences of up to 4096 keys, 32 heads over 8 (195 MB) 43 us and 5 for the joins, 4.6 TB/s; four of up to 131072 keys, 8 heads over one
 // (75 MB) 20 and 6 us, of which 4 and 2.5 are launch and latency; one of 876 keys 7.4 and 3: a chain of lengths, page, cache and parts.  A unit is 4 waves x 64 keys; each wave keeps its own state and shares nothing before the end of an item.
 //
@@ -552,10 +557,16 @@ int launch_cache_attn_wide(const slimattn_cache_params& p, int n_q_heads, AttnAr
 namespace {
 
 // Which kernel takes a sequence goes by its number of query columns, which the device knows (row_ptr): the narrow kernel's time grows with the
-// tiles of 16, the wide one's steps up every 256.  d 128, 32 heads over 8, us narrow / wide at 64, 96, 128 columns a sequence, caches in rotation: 16 of 4K keys
-// 69 / 91, 71 / 92, 109 / 93; 64 of 4K 218 / 283, 264 / 305, 384 / 293; 128 of 1K 137 / 168, 170 / 172, 233 / 177; at 64, 128, 256, 512 columns, one cache: one sequence of
-// 32K keys 39 / 60, 61 / 61, 92 / 66, 159 / 98; eight of 4K 42 / 60, 63 / 63, 103 / 71, 178 / 108.  Where there is little to do (8K keys, two heads) the
-// wide kernel's larger parts cost more than it saves, up to 512 columns: 21 / 32, 35 / 38.
+// tiles of 16, the wide one's steps up every 256.  us narrow / wide, caches in rotation (as far as memory allows), columns a sequence:
+//                                            64           96          112          128          192
+//   64 of 4K keys, 32 heads over 8, d 128   216 /  287   272 /  309   344 /  303   380 /  297   497 /  311
+//   16 of 4K                                 68 /   91    67 /   93   101 /   95   105 /   95   126 /  101
+//   1 of 32K                                 36 /   56    43 /   57    53 /   58    57 /   57    73 /   60
+//   64 of 4K, 32 heads over 32              873 / 1122  1244 / 1157  1450 / 1187  1646 / 1191  2383 / 1236
+//   64 of 4K, 8 heads over one               40 /   61    49 /   63    59 /   64    66 /   65    67 /   68
+//   64 of 4K, 32 heads over 8, d 64         108 /  203   153 /  204   205 /  207   198 /  207   294 /  211
+// 64 heads over 8 go as 32 over 8.  Where there is little to do the rule costs time, since the wide kernel's larger parts take more than it saves: at 128 columns
+// 1 of 32K keys over one head 22 / 34, 16 of 4K over one 28 / 38, 1 of 8K over 8 29 / 33 (d 64: 24 / 24).
 constexpr long long kNarrowCols = 112;
 bool may_be_wide(const slimattn_cache_params& p, int n_q_heads, bool ragged) {
   return p.dtype == SLIMATTN_BF16 && (ragged ? p.n_rows : 1ll) * (n_q_heads / p.n_kv_heads) > kNarrowCols;
@@ -595,9 +606,9 @@ int launch_cache_attn(const slimattn_cache_params& p, int n_q_heads, float scale
   // save: eight of 131072 (96) 39.4 / 39.8, sixteen of 32768 (48) 26.0 / 26.6, fp32 of 65536 keys over 8 heads of 64 (96) 23.5 / 24.6.
   const bool many = a.slots && blocks >= 128 * a.slots;
   // Where sequences have 16 columns or fewer on average, their keys are read by one tile each and by nobody before the next call, with the other
-  // layers' caches in between: streamed.  Caches in rotation, d 128, 32 heads over 8, us without / with: 19 MB 18.4 / 17.3, 76 MB 27.4 / 25.4, 303 MB
-  // 76.9 / 65.9, 606 MB 133 / 115; 64 columns a sequence (four tiles) 222 / 229; a single cache read again and again from the last-level
-  // cache 51.2 / 52.9.
+  // layers' caches in between: streamed.  Caches in rotation, d 128, 32 heads over 8, us without / with: 19 MB 17.2 / 15.8, 76 MB 27.9 / 25.6, 303 MB
+  // 78.6 / 67.4, 606 MB 132 / 116; 64 columns a sequence (four tiles) 223 / 234; a single cache of 195 MB read again and again from the last-level
+  // cache 53.0 / 54.7.  (The host knows the average alone: a prompt among single tokens has all of them read through the caches.)
   const bool once = (long long)p.n_rows * a.group <= (long long)kCols * p.n_seqs;
   auto run = [&](auto t, auto d) {
     using T = decltype(t);

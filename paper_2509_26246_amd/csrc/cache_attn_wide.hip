@@ -6,7 +6,10 @@
 // columns (a lane holds one column's scores, so sums and maxima need one lane exchange), tiles are double-buffered, and the next tile's codes are loaded
 // a tile ahead of that and unpacked beside the products of this one.  LDS rows are padded, so that a fragment is one address and a constant.
 //
-// 1024 new rows behind 31K keys, 8 heads over one, head dim 128 (135 GFLOP): 157 us in all, 860 TFLOP/s; the narrow kernel takes 293 us.  A tile of 64 keys
+// Probabilities are rounded to bf16 for the second product, as slimattn_fwd rounds them (at most 2^-8 of each term; the sum takes them unrounded): a
+// second term would make that product two, half as much again of all the matrix work, for an error of 1.65e-3 instead of 2.3e-3 (cache_attn.hip).
+//
+// 1024 new rows behind 31K keys, 8 heads over one, head dim 128 (135 GFLOP): 157 to 165 us in all, 820 to 860 TFLOP/s; the narrow kernel takes 293 us.  A tile of 64 keys
 // takes a compute unit 2 us (1050 TFLOP/s; a large library product reaches 1220), the rest is fixed: finding the work, first loads, parts, join.  No
 // single part binds a tile: matrix unit 43% of the cycles, vector unit 50%, LDS 45%; without the exponentials, the second product, the unpacking
 // or the loads (each taken out alone) 5 to 8% go.  Within 4% of it came four waves of 32 columns, two blocks to a compute unit, and four waves of 64
