@@ -494,7 +494,7 @@ int slimattn_cache_read(const slimattn_cache_params* p, const void* cache, const
 size_t slimattn_cache_attn_workspace_bytes(const slimattn_cache_params* p, int32_t n_q_heads);
 
 /* Attention of the rows over their sequences' caches: the row at position p sees keys 0 .. p,
- * S_j = scale * q . k_j, lse = log sum_j exp S_j, o = sum_j exp(S_j - lse) v_j.  q, o [n_rows, Hq, d] packed, Hq a multiple of Hkv (query head h
+ * S_j = scale * q . k_j (scale between -2^127 and 2^127), lse = log sum_j exp S_j, o = sum_j exp(S_j - lse) v_j.  q, o [n_rows, Hq, d] packed, Hq a multiple of Hkv (query head h
  * uses KV head h / (Hq / Hkv)); lse float [Hq, n_rows] or NULL.  The keys of long sequences are divided among blocks
  * and the parts added in their order: the same call on the same inputs gives the same bits.  Statistics and sums are fp32; with SLIMATTN_BF16 the probabilities
  * (times the values' scales) are rounded to bf16 for the product with the values, as in slimattn_fwd: o is within 2^-8 of the largest |v| by that, beside its own rounding.  Sequences of

@@ -106,7 +106,7 @@ int slimattn_cache_attn(const slimattn_cache_params* p, int32_t n_q_heads, float
                         void* stream) {
   int rc = check(p);
   if (rc != SLIMATTN_OK) return rc;
-  if (!heads_ok(p, n_q_heads) || !(scale - scale == 0.f)) return SLIMATTN_EINVAL;
+  if (!heads_ok(p, n_q_heads) || !(scale >= -0x1p127f && scale <= 0x1p127f)) return SLIMATTN_EINVAL;   // times log2 e it is finite
   if (p->n_rows == 0 || p->n_seqs == 0) return SLIMATTN_OK;
   rc = check_arrays(p, row_ptr, lens, page_table);
   if (rc != SLIMATTN_OK) return rc;

@@ -157,3 +157,12 @@ ARRAYS = [("lens", 0), ("lens", 12), ("page_table", 60), ("row_ptr", 16)]
                                                   dict(workspace=("q", 0)), dict(workspace=("cache", 0)), dict(o=("cache", 64)), dict(lse=("cache", 0)), dict(o=("q", 16)))], ids=str)
 def test_cache_calls_refuse_outputs_over_anything(call, over):
     _overlaps_cache(call, over)
+
+
+@pytest.mark.parametrize("scale", [3.4e38, -3.0e38, 1.8e38, float("inf"), float("nan")])
+def test_scales_beyond_the_exponentials_units_are_refused(scale):
+    # the kernels work in units of log 2: a finite scale whose product with log2 e is not made every row NaN; the limit is 2^127 = 1.7e38
+    ptr = {n: (i + 1) * A for i, n in enumerate(("q", "cache", "page_table", "lens", "o", "lse", "workspace"))}
+    with pytest.raises(S.SlimAttnError) as e:
+        S.cache_attn(*ptr.values(), n_q_heads=HQ, scale=scale, **CACHE)
+    assert e.value.code == -1
